@@ -23,22 +23,12 @@
 #include <mutex>
 #include <type_traits>
 
+#include "device.hpp"
 #include "plan.hpp"
 
 namespace c2kv {
 
-typedef __bf16 bf16x8 __attribute__((__vector_size__(8 * sizeof(__bf16))));
-typedef float f32x16 __attribute__((__vector_size__(16 * sizeof(float))));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-
 constexpr int KT = kKeyTile;
-constexpr float kNegInf = -__builtin_huge_valf();
-constexpr float kLazyLog2 = 8.f;  // reference-maximum slack of the bf16 online softmax
-constexpr float kLn2 = 0.693147180559945309f;
-// fourth descriptor word of a raw (unformatted, unswizzled) buffer on gfx9-family
-// parts; reads past num_records return zero
-constexpr int kBufferFlags = 0x00020000;
 // row blocks (of at most 128 rows) with more splits than this are merged one
 // row per workgroup
 constexpr int kSplitMergeMin = 16;
@@ -47,188 +37,6 @@ constexpr int kSplitMergeMin = 16;
 // suffix instead of the causal one (its own kernels, so that the causal ones
 // carry none of the SIF mask's registers)
 enum Src { SRC_PAGED = 0, SRC_POOL = 1, SRC_POOL_I8 = 2, SRC_PAGED_SIF = 3 };
-
-// ----------------------------------------------------------------------------
-// element helpers
-// ----------------------------------------------------------------------------
-
-__device__ inline float to_f(float x) { return x; }
-__device__ inline float to_f(__bf16 x) { return static_cast<float>(x); }
-
-template <typename T> __device__ inline T from_f(float x);
-template <> __device__ inline float from_f<float>(float x) { return x; }
-template <> __device__ inline __bf16 from_f<__bf16>(float x) { return static_cast<__bf16>(x); }
-
-// 8 consecutive elements -> float
-__device__ inline void load8(const float* p, float (&x)[8]) {
-  const float4 a = *reinterpret_cast<const float4*>(p);
-  const float4 b = *reinterpret_cast<const float4*>(p + 4);
-  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-  x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-}
-__device__ inline void load8(const __bf16* p, float (&x)[8]) {
-  const uint4 u = *reinterpret_cast<const uint4*>(p);
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(w[i] << 16);
-    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
-}
-__device__ inline void load8(const int8_t* p, float (&x)[8]) {
-  const uint2 u = *reinterpret_cast<const uint2*>(p);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[i] = static_cast<float>(static_cast<int8_t>((u.x >> (8 * i)) & 0xff));
-    x[4 + i] = static_cast<float>(static_cast<int8_t>((u.y >> (8 * i)) & 0xff));
-  }
-}
-
-// 8 floats -> 8 consecutive T (16-byte aligned destination for bf16)
-__device__ inline void store8(float* p, const float (&x)[8]) {
-  *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
-  *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
-}
-// (a, b) -> bf16 pair, a in the low half: one paired round-to-nearest-even
-// conversion (two scalar conversions would each need a shift or merge after)
-__device__ inline uint32_t pack_bf16(float a, float b) {
-  const f32x2 v = {a, b};
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
-}
-__device__ inline void store8(__bf16* p, const float (&x)[8]) {
-  uint4 u;
-  u.x = pack_bf16(x[0], x[1]);
-  u.y = pack_bf16(x[2], x[3]);
-  u.z = pack_bf16(x[4], x[5]);
-  u.w = pack_bf16(x[6], x[7]);
-  *reinterpret_cast<uint4*>(p) = u;
-}
-template <typename T>
-__device__ inline void store8_zero(T* p) {
-  if constexpr (sizeof(T) == 4) {
-    *reinterpret_cast<float4*>(p) = make_float4(0.f, 0.f, 0.f, 0.f);
-    *reinterpret_cast<float4*>(p + 4) = make_float4(0.f, 0.f, 0.f, 0.f);
-  } else {
-    *reinterpret_cast<uint4*>(p) = make_uint4(0u, 0u, 0u, 0u);
-  }
-}
-
-// cos/sin of 8 consecutive frequencies (float2 pairs)
-__device__ inline void load_cs8(const float2* cs, float (&c)[8], float (&s)[8]) {
-  const float4* p = reinterpret_cast<const float4*>(cs);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float4 v = p[i];
-    c[2 * i] = v.x; s[2 * i] = v.y; c[2 * i + 1] = v.z; s[2 * i + 1] = v.w;
-  }
-}
-
-// Half-split RoPE turn of the pair (x_i, x_{i+D/2}) by the angle whose cos/sin
-// are given (x <- x c - y s, y <- x s + y c).  The fused multiply-adds are
-// written out so that every kernel rounds a turned key the same way.
-__device__ inline void rotate_pair(float& x, float& y, float c, float s) {
-  const float a = x, b = y;
-  x = __builtin_fmaf(a, c, -(b * s));
-  y = __builtin_fmaf(a, s, b * c);
-}
-__device__ inline void rotate8(float (&x)[8], float (&y)[8], const float (&c)[8],
-                               const float (&s)[8]) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) rotate_pair(x[e], y[e], c[e], s[e]);
-}
-
-// ----------------------------------------------------------------------------
-// MFMA traits: bf16 32x32x16 (8 k per lane) and f32 32x32x2 (1 k per lane)
-// ----------------------------------------------------------------------------
-
-template <typename T> struct Mma;
-template <> struct Mma<float> {
-  static constexpr int KPL = 1;
-  using Op = float;
-  __device__ static inline f32x16 run(Op a, Op b, f32x16 c) {
-    return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
-  }
-};
-template <> struct Mma<__bf16> {
-  static constexpr int KPL = 8;
-  using Op = bf16x8;
-  __device__ static inline f32x16 run(Op a, Op b, f32x16 c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
-  }
-};
-
-// maximum of x over lanes l and l ^ 32, a VALU lane swap: the swap's first
-// result holds the lower half's values in every lane, the second the upper's
-__device__ inline float half_pair_max(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
-                                                  false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-
-// sum of x over lanes l and l ^ 32, the same value (same operand order) in both
-__device__ inline float half_pair_sum(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
-                                                  false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
-// ----------------------------------------------------------------------------
-// raw 32-bit words of 8 consecutive elements (2 * sizeof(S) words)
-// ----------------------------------------------------------------------------
-
-template <typename S>
-__device__ inline void raw_load8(uint32_t* w, const S* p) {
-  if constexpr (sizeof(S) == 4) {
-    const uint4 u0 = *reinterpret_cast<const uint4*>(p);
-    const uint4 u1 = *reinterpret_cast<const uint4*>(p + 4);
-    w[0] = u0.x; w[1] = u0.y; w[2] = u0.z; w[3] = u0.w;
-    w[4] = u1.x; w[5] = u1.y; w[6] = u1.z; w[7] = u1.w;
-  } else if constexpr (sizeof(S) == 2) {
-    const uint4 u0 = *reinterpret_cast<const uint4*>(p);
-    w[0] = u0.x; w[1] = u0.y; w[2] = u0.z; w[3] = u0.w;
-  } else {
-    const uint2 u0 = *reinterpret_cast<const uint2*>(p);
-    w[0] = u0.x; w[1] = u0.y;
-  }
-}
-template <typename S>
-__device__ inline void raw_zero8(uint32_t* w) {
-#pragma unroll
-  for (int i = 0; i < 2 * int(sizeof(S)); ++i) w[i] = 0u;
-}
-template <typename S>
-__device__ inline void raw_to_f8(const uint32_t* w, float (&x)[8]) {
-  if constexpr (sizeof(S) == 4) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]);
-  } else if constexpr (sizeof(S) == 2) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(w[i] << 16);
-      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      x[i] = static_cast<float>(static_cast<int8_t>((w[i >> 2] >> (8 * (i & 3))) & 0xffu));
-  }
-}
-
-// zero the elements [n_keep, 16 / sizeof(T)) of a 16-byte vector (a mask per
-// word from selects, no branches: n_keep differs between lanes)
-template <typename T>
-__device__ inline uint4 keep_first(uint4 v, int n_keep) {
-  uint32_t w[4] = {v.x, v.y, v.z, v.w};
-  constexpr int EPW = 4 / sizeof(T);              // elements per word
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int k = n_keep - EPW * i;               // elements of word i to keep
-    uint32_t m = k >= EPW ? 0xffffffffu : 0u;
-    if constexpr (EPW == 2) m = k == 1 ? 0x0000ffffu : m;
-    w[i] &= m;
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
 
 // ----------------------------------------------------------------------------
 // parameters
@@ -1970,17 +1778,6 @@ hipError_t static_scratch(void** out) {
 }
 
 namespace {
-
-// Launch `kernel(params)`.  With timing events, the dispatch packet itself
-// stamps them at kernel start and end (hipExtLaunchKernel), the same
-// timestamps a kernel trace reports.
-template <typename P>
-hipError_t launch(const void* kernel, dim3 grid, dim3 block, hipStream_t st, const P& params,
-                  hipEvent_t ev0, hipEvent_t ev1) {
-  void* args[] = {const_cast<P*>(&params)};
-  if (ev0 || ev1) return hipExtLaunchKernel(kernel, grid, block, args, 0, st, ev0, ev1, 0);
-  return hipLaunchKernel(kernel, grid, block, args, 0, st);
-}
 
 template <typename T>
 const T* at(const void* base, size_t off) {

@@ -112,10 +112,7 @@ struct Work {
 
 }  // namespace
 
-c2kv_status build_plan(const c2kv_attn_cfg& cfg, const c2kv_compose_desc& d,
-                       int32_t suffix_len, const c2kv_plan_opts* opts, Plan& p,
-                       std::string& err, const SifShape* sif) {
-  // ---- attention shape ----------------------------------------------------
+c2kv_status check_cfg(const c2kv_attn_cfg& cfg, std::string& err) {
   if (cfg.n_q_heads < 1 || cfg.n_kv_heads < 1 || cfg.n_q_heads % cfg.n_kv_heads != 0) {
     err = fmt("n_q_heads (", cfg.n_q_heads, ") must be a positive multiple of n_kv_heads (",
               cfg.n_kv_heads, ")");
@@ -141,6 +138,13 @@ c2kv_status build_plan(const c2kv_attn_cfg& cfg, const c2kv_compose_desc& d,
     err = "softmax_scale must be finite";
     return C2KV_E_INVAL;
   }
+  return C2KV_OK;
+}
+
+c2kv_status build_plan(const c2kv_attn_cfg& cfg, const c2kv_compose_desc& d,
+                       int32_t suffix_len, const c2kv_plan_opts* opts, Plan& p,
+                       std::string& err, const SifShape* sif) {
+  if (const c2kv_status st = check_cfg(cfg, err); st != C2KV_OK) return st;
   if (suffix_len < 1) {
     err = fmt("suffix_len must be >= 1, got ", suffix_len);
     return C2KV_E_INVAL;

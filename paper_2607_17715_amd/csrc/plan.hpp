@@ -105,6 +105,9 @@ struct Plan {
 // n_tokens original tokens followed by one C^2 token per block of `block` tokens.
 struct SifShape { int32_t n_tokens, block, sink; };
 
+// The checks of an attention shape, shared by plans and the cache calls.
+c2kv_status check_cfg(const c2kv_attn_cfg& cfg, std::string& err);
+
 // Builds the plan; returns C2KV_OK or an error with `err` set.  With `sif`, the
 // request has no segments and its suffix is the SIF sequence.
 c2kv_status build_plan(const c2kv_attn_cfg& cfg, const c2kv_compose_desc& desc,

@@ -299,11 +299,104 @@ c2kv_status c2kv_host_free(void* host);
 c2kv_status c2kv_load(const c2kv_plan* plan, const c2kv_pool* src, const c2kv_pool* dst,
                       void* stream);
 
+/* ---- the growing cache ------------------------------------------------------
+ * After the composed context, the prompt's and the generated tokens enter the cache:
+ * c2kv_cache_write puts their keys and values into pages, c2kv_cache_attend lets them
+ * attend (a prompt in chunks, drafted tokens, one token a step), c2kv_cache_read brings
+ * cached tokens back as rows, and c2kv_pool_write stores rows in a chunk pool, where
+ * plans find them.  The cache may be the pages that c2kv_compose wrote (k_pages and
+ * v_pages, its block table widened by the pages that the new tokens fill) or one of
+ * int8.  These calls need no plan: lengths, offsets and pages are DEVICE arrays, read
+ * when the kernels run, so that a captured step can be replayed while they grow.
+ *
+ * What a device array names outside the buffers is left alone: a token whose cache
+ * index is negative, lies beyond its block-table row, or is on a page outside
+ * [0, n_pages) (-1: no page) is not written, not read back (its row stays as it was)
+ * and, as a key, is not there.  Row i of the chunk tensors belongs to request b where
+ * tok_off[b] <= i < tok_off[b+1]; rows that belong to none stay as they were.
+ *
+ * Alignment: pages, pools, scales, q, k, v and out lie on 16 bytes, and so do all
+ * their tokens (strides).  C2KV_E_INVAL otherwise. */
+
+/* A paged cache of one layer: caller-owned device memory, in the layout of
+ * c2kv_compose's pages.  Storage F32 with F32 activations, BF16 or I8 with BF16. */
+typedef struct c2kv_cache {
+  c2kv_dtype dtype;        /* storage dtype: F32, BF16 or I8                       */
+  void* k;                 /* [n_pages][H_kv][page_size][D]                        */
+  void* v;                 /* [n_pages][H_kv][D][page_size], TRANSPOSED in a page  */
+  float* k_scale;          /* [n_pages][H_kv][page_size], I8 only (else NULL)      */
+  float* v_scale;          /* [n_pages][H_kv][page_size], I8 only (else NULL)      */
+  int32_t n_pages;
+  int32_t page_size;       /* tokens per page, a multiple of 64                    */
+} c2kv_cache;
+
+/* The chunk of tokens of each request that a call is about: the last
+ * n_b = tok_off[b+1] - tok_off[b] of its kv_len[b] cached tokens.  Token t of the chunk
+ * is row tok_off[b] + t of the call's tensors and cache index j = kv_len[b] - n_b + t,
+ * at offset j % page_size of page block_table[b][j / page_size].  For a step of new
+ * tokens kv_len counts them; to read a whole cache back, n_b = kv_len[b]. */
+typedef struct c2kv_chunks {
+  int32_t batch;               /* B >= 1                                           */
+  int32_t n_tokens;            /* rows of the chunk tensors, at least tok_off[B]   */
+  const int32_t* tok_off;      /* [B+1] DEVICE, ascending                          */
+  const int32_t* kv_len;       /* [B] DEVICE                                       */
+  const int32_t* block_table;  /* [B][max_pages] DEVICE                            */
+  int32_t max_pages;           /* columns of the block table, >= 1                 */
+  int32_t max_chunk;           /* a bound on n_b and one on kv_len, for launch     */
+  int32_t max_kv;              /* shapes only (any value gives the same results;
+                                  0: n_tokens and max_pages * page_size)           */
+} c2kv_chunks;
+
+/* Write each chunk's tokens into the cache.  k, v [n_tokens][H_kv][D] in the act dtype,
+ * k_stride and v_stride elements between tokens (0: H_kv * D), so that they may be
+ * columns of one projection's output.  pos [n_tokens] DEVICE: k is not yet
+ * RoPE-encoded and is turned to these positions; NULL: k is written as it is.  I8:
+ * symmetric per (token, kv-head), scale = max|x| / 127 (1 for zeros) of the turned key
+ * in fp32, code = x / scale to the nearest, ties to even; a row that holds an infinity
+ * or a NaN reads back as NaN.  Two tokens of one call must not have the same place. */
+c2kv_status c2kv_cache_write(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,
+                             const c2kv_chunks* chunks, const void* k, int64_t k_stride,
+                             const void* v, int64_t v_stride, const int32_t* pos,
+                             void* stream);
+
+/* Read each chunk's tokens back as rows: k, v [n_tokens][H_kv][D] in the act dtype,
+ * I8 decoded (code * scale in fp32).  turn [n_tokens] DEVICE turns key i by turn[i]
+ * positions (minus its position gives the key before RoPE); NULL: keys as cached. */
+c2kv_status c2kv_cache_read(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,
+                            const c2kv_chunks* chunks, const int32_t* turn, void* k, void* v,
+                            void* stream);
+
+/* Attention of each chunk's tokens over its request's cache, which holds them already:
+ * token t of request b sees cache indices j <= kv_len[b] - n_b + t.  q [n_tokens][H_q][D]
+ * with q_stride elements between tokens (0: H_q * D), turned to pos as in
+ * c2kv_cache_write (NULL: as it is).  out [n_tokens][H_q][D], lse [n_tokens][H_q] float32
+ * natural-log (NULL to skip).  A token that sees no key gets zeros and an lse of -inf;
+ * what lies in pages behind the last cached token has no effect, whatever it is.
+ * workspace: device memory on 256 bytes, of c2kv_cache_attend_workspace's size; calls
+ * that share one must be ordered.  It need not be cleared. */
+c2kv_status c2kv_cache_attend_workspace(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,
+                                        const c2kv_chunks* chunks, size_t* bytes);
+c2kv_status c2kv_cache_attend(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,
+                              const c2kv_chunks* chunks, const void* q, int64_t q_stride,
+                              const int32_t* pos, void* out, float* lse, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/* Store n rows in a chunk pool: row i goes to pool row row[i] (DEVICE; rows outside
+ * [0, n_rows) are skipped), K and V in the pool's dtype (I8: as c2kv_cache_write, the
+ * scales to pool->k_scale and v_scale).  pos [n] DEVICE encodes k at these positions
+ * (c2kv_key_encoding C2KV_KEYS_ROPE_AT_ORIG: seg_orig_pos0 + j); NULL stores it as it is.
+ * pool is written; two rows of one call must not have the same place. */
+c2kv_status c2kv_pool_write(const c2kv_attn_cfg* cfg, const c2kv_pool* pool, int32_t n,
+                            const int64_t* row, const void* k, int64_t k_stride,
+                            const void* v, int64_t v_stride, const int32_t* pos,
+                            void* stream);
+
 /* Per-kernel timing for measurement: when enabled, every kernel is launched
  * with a pair of HIP events that its dispatch stamps at kernel start and end
  * (on the kernel's own stream).  c2kv_timing_read synchronises on them and
  * returns the summed milliseconds and launch count of kernel `name`
- * ("compose", "attn_paged", "attn_pool", "merge") since the last reset.
+ * ("compose", "attn_paged", "attn_pool", "merge", "cache_write", "cache_read",
+ * "cache_attend", "cache_merge", "pool_write") since the last reset.
  * Launches with timing on are not meant for graph capture. */
 c2kv_status c2kv_timing_enable(int32_t on);
 c2kv_status c2kv_timing_reset(void);

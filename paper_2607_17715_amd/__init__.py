@@ -31,6 +31,8 @@ EXPORTED = [
     "c2kv_attend", "c2kv_compose_attend", "c2kv_timing_enable", "c2kv_timing_reset",
     "c2kv_timing_read", "c2kv_last_error", "c2kv_version", "c2kv_host_alloc",
     "c2kv_host_free", "c2kv_load", "c2kv_sif_plan_create", "c2kv_compose_attend_static",
+    "c2kv_cache_write", "c2kv_cache_read", "c2kv_cache_attend_workspace", "c2kv_cache_attend",
+    "c2kv_pool_write",
 ]
 STATIC_SCRATCH_BYTES = 32 << 20   # C2KV_STATIC_SCRATCH_BYTES
 
@@ -66,6 +68,19 @@ class PoolDesc(ctypes.Structure):
     _fields_ = [("dtype", ctypes.c_int32), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
                 ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
                 ("n_rows", ctypes.c_int64)]
+
+
+class CacheDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32)]
+
+
+class ChunksDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("n_tokens", ctypes.c_int32),
+                ("tok_off", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+                ("block_table", ctypes.c_void_p), ("max_pages", ctypes.c_int32),
+                ("max_chunk", ctypes.c_int32), ("max_kv", ctypes.c_int32)]
 
 
 class PlanInfo(ctypes.Structure):
@@ -108,6 +123,12 @@ def _load() -> ctypes.CDLL:
         "c2kv_host_free": [vp],
         "c2kv_load": [vp, P(PoolDesc), P(PoolDesc), vp],
         "c2kv_sif_plan_create": [P(AttnCfg), i32, i32, i32, i32, P(PlanOpts), P(vp)],
+        "c2kv_cache_write": [P(AttnCfg), P(CacheDesc), P(ChunksDesc), vp, i64, vp, i64, vp, vp],
+        "c2kv_cache_read": [P(AttnCfg), P(CacheDesc), P(ChunksDesc), vp, vp, vp, vp],
+        "c2kv_cache_attend_workspace": [P(AttnCfg), P(CacheDesc), P(ChunksDesc), P(sz)],
+        "c2kv_cache_attend": [P(AttnCfg), P(CacheDesc), P(ChunksDesc), vp, i64, vp, vp, vp, vp,
+                              sz, vp],
+        "c2kv_pool_write": [P(AttnCfg), P(PoolDesc), i32, vp, vp, i64, vp, i64, vp, vp],
     }
     for name, args in sig.items():
         f = getattr(lib, name)
@@ -283,8 +304,10 @@ def pool_desc(k, v, k_scale=None, v_scale=None) -> PoolDesc:
     code = {torch.float32: C2KV_F32, torch.bfloat16: C2KV_BF16, torch.int8: C2KV_I8}[k.dtype]
     if v.dtype != k.dtype or v.shape != k.shape:
         raise ValueError("pool K and V must have the same dtype and shape")
-    return PoolDesc(code, _dev_ptr(k), _dev_ptr(v), _dev_ptr(k_scale), _dev_ptr(v_scale),
+    desc = PoolDesc(code, _dev_ptr(k), _dev_ptr(v), _dev_ptr(k_scale), _dev_ptr(v_scale),
                     int(k.shape[0]))
+    desc.row_shape, desc.device = tuple(k.shape[1:]), k.device
+    return desc
 
 
 def page_shapes(plan: Plan):
@@ -325,6 +348,211 @@ def c2kv_compose_attend_static(plan: Plan, pool: PoolDesc, q, k_suf, v_suf, out,
 
 def c2kv_load(plan: Plan, src: PoolDesc, dst: PoolDesc, stream=None):
     _check(_lib.c2kv_load(plan.handle, ctypes.byref(src), ctypes.byref(dst), _stream(stream)))
+
+
+# ---- the growing cache ---------------------------------------------------------
+
+def attn_cfg(n_q_heads: int, n_kv_heads: int, head_dim: int, act_dtype: str, rope_base: float,
+             softmax_scale: float = 0.0) -> AttnCfg:
+    """Attention shape of the cache calls and c2kv_pool_write (a plan makes its own)."""
+    return AttnCfg(n_q_heads, n_kv_heads, head_dim, _DTYPE_CODE[act_dtype], float(rope_base),
+                   float(softmax_scale))
+
+
+class Cache:
+    """A paged cache of one layer (c2kv_cache): k [n_pages][H_kv][page_size][D],
+    v [n_pages][H_kv][D][page_size], for int8 with scales [n_pages][H_kv][page_size]."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        import torch
+        code = {torch.float32: C2KV_F32, torch.bfloat16: C2KV_BF16, torch.int8: C2KV_I8}[k.dtype]
+        n_pages, heads, page, d = k.shape
+        if v.dtype != k.dtype or tuple(v.shape) != (n_pages, heads, d, page):
+            raise ValueError("v must have k's dtype and each page transposed")
+        for s in (k_scale, v_scale):
+            if s is not None and (s.dtype != torch.float32 or
+                                  tuple(s.shape) != (n_pages, heads, page)):
+                raise ValueError("scales must be float32 [n_pages][H_kv][page_size]")
+        self.tensors = (k, v, k_scale, v_scale)
+        self.device = _one_device(*self.tensors)
+        self.heads, self.head_dim = heads, d
+        self.desc = CacheDesc(code, *(_dev_ptr(t) for t in self.tensors), n_pages, page)
+        self.ref = ctypes.byref(self.desc)
+
+
+class Chunks:
+    """The chunk of each request of a batch (c2kv_chunks): tok_off [B+1], kv_len [B] and
+    block_table [B][max_pages], int32 on the device, read when the kernels run; n_tokens
+    rows in the tensors of a call; max_chunk and max_kv bound the lengths (0: unknown)."""
+
+    def __init__(self, tok_off, kv_len, block_table, n_tokens: int, max_chunk: int = 0,
+                 max_kv: int = 0):
+        import torch
+        batch, max_pages = block_table.shape
+        if any(t.dtype != torch.int32 for t in (tok_off, kv_len, block_table)):
+            raise ValueError("tok_off, kv_len and block_table must be int32")
+        if tuple(tok_off.shape) != (batch + 1,) or tuple(kv_len.shape) != (batch,):
+            raise ValueError("tok_off must have B + 1 entries and kv_len B")
+        self.tensors = (tok_off, kv_len, block_table)
+        self.device = _one_device(*self.tensors)
+        self.n_tokens = int(n_tokens)
+        self.desc = ChunksDesc(batch, self.n_tokens, *(_dev_ptr(t) for t in self.tensors),
+                               max_pages, int(max_chunk), int(max_kv))
+        self.ref = ctypes.byref(self.desc)
+
+
+def _one_device(*tensors):
+    devices = {t.device for t in tensors if t is not None}
+    if len(devices) != 1:
+        raise ValueError(f"tensors on different devices: {sorted(map(str, devices))}")
+    return devices.pop()
+
+
+class _on:
+    """The current device is `device` inside, whatever it was: a call's stream and
+    kernels are of the device that its tensors are on."""
+
+    def __init__(self, device):
+        import torch
+        self._guard = (None if device.index == torch.cuda.current_device()
+                       else torch.cuda.device(device))
+
+    def __enter__(self):
+        if self._guard is not None:
+            self._guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self._guard is not None:
+            self._guard.__exit__(*exc)
+
+
+_ACT = {}
+
+
+def _rows(t, cfg: AttnCfg, heads: int, n: int, device, what: str):
+    """Pointer and token stride of rows [n][heads][D]: tokens may lie apart, a token is dense."""
+    if not _ACT:
+        import torch
+        _ACT.update({C2KV_F32: torch.float32, C2KV_BF16: torch.bfloat16})
+    if t.dim() != 3 or t.shape[0] < n or t.shape[1] != heads or t.shape[2] != cfg.head_dim:
+        raise ValueError(f"{what} must be [{n}][{heads}][{cfg.head_dim}], got {list(t.shape)}")
+    if t.dtype is not _ACT.get(cfg.act_dtype) or t.device != device:
+        raise ValueError(f"{what} must have the act dtype and lie on {device}, "
+                         f"got {t.dtype} on {t.device}")
+    s0, s1, s2 = t.stride()
+    if s2 != 1 or s1 != cfg.head_dim and heads > 1:
+        raise ValueError(f"the heads of {what} must be dense")
+    return t.data_ptr(), s0 if t.shape[0] > 1 else 0
+
+
+def _dense(t, cfg: AttnCfg, heads: int, n: int, device, what: str):
+    if not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+    return _rows(t, cfg, heads, n, device, what)[0]
+
+
+def _index(t, dtype, n: int, device, what: str):
+    if t is None:
+        return None
+    if t.dtype != dtype or t.dim() != 1 or t.shape[0] < n or t.device != device \
+            or not t.is_contiguous():
+        raise ValueError(f"{what} must be {dtype} [{n}], contiguous, on {device}")
+    return t.data_ptr()
+
+
+def _of(cfg: AttnCfg, cache: Cache, chunks: Chunks):
+    if cache.heads != cfg.n_kv_heads or cache.head_dim != cfg.head_dim:
+        raise ValueError(f"the cache has {cache.heads} heads of {cache.head_dim}, the shape "
+                         f"{cfg.n_kv_heads} of {cfg.head_dim}")
+    if cache.device != chunks.device:
+        raise ValueError(f"cache on {cache.device}, chunks on {chunks.device}")
+    return cache.device, chunks.n_tokens
+
+
+def c2kv_cache_write(cfg: AttnCfg, cache: Cache, chunks: Chunks, k, v, pos=None, stream=None):
+    """Put the chunks' tokens into the cache; pos [n_tokens] int32: k is turned to these
+    positions (None: written as it is)."""
+    import torch
+    dev, n = _of(cfg, cache, chunks)
+    kp, ks = _rows(k, cfg, cfg.n_kv_heads, n, dev, "k")
+    vp, vs = _rows(v, cfg, cfg.n_kv_heads, n, dev, "v")
+    pos = _index(pos, torch.int32, n, dev, "pos")
+    with _on(dev):
+        _check(_lib.c2kv_cache_write(ctypes.byref(cfg), cache.ref, chunks.ref, kp, ks, vp, vs,
+                                     pos, _stream(stream)))
+
+
+def c2kv_cache_read(cfg: AttnCfg, cache: Cache, chunks: Chunks, k, v, turn=None, stream=None):
+    """The chunks' tokens as rows k and v [n_tokens][H_kv][D]; turn [n_tokens] int32 turns
+    key i by turn[i] positions."""
+    import torch
+    dev, n = _of(cfg, cache, chunks)
+    kp = _dense(k, cfg, cfg.n_kv_heads, n, dev, "k")
+    vp = _dense(v, cfg, cfg.n_kv_heads, n, dev, "v")
+    turn = _index(turn, torch.int32, n, dev, "turn")
+    with _on(dev):
+        _check(_lib.c2kv_cache_read(ctypes.byref(cfg), cache.ref, chunks.ref, turn, kp, vp,
+                                    _stream(stream)))
+
+
+def cache_attend_workspace(cfg: AttnCfg, cache: Cache, chunks: Chunks):
+    """A workspace for c2kv_cache_attend calls of this shape that are ordered."""
+    import torch
+    nbytes = ctypes.c_size_t()
+    _check(_lib.c2kv_cache_attend_workspace(ctypes.byref(cfg), cache.ref, chunks.ref,
+                                            ctypes.byref(nbytes)))
+    raw = torch.empty(nbytes.value + 256, dtype=torch.uint8, device=cache.device)
+    off = (-raw.data_ptr()) % 256
+    return raw[off:off + nbytes.value]
+
+
+def c2kv_cache_attend(cfg: AttnCfg, cache: Cache, chunks: Chunks, q, out, pos=None, lse=None,
+                      workspace=None, stream=None):
+    """Causal attention of the chunks' queries over their requests' caches; pos [n_tokens]
+    int32 turns q (None: as it is); lse [n_tokens][H_q] float32; workspace: from
+    cache_attend_workspace (allocated for the call, on the current stream, if not given)."""
+    import torch
+    dev, n = _of(cfg, cache, chunks)
+    qp, qs = _rows(q, cfg, cfg.n_q_heads, n, dev, "q")
+    op = _dense(out, cfg, cfg.n_q_heads, n, dev, "out")
+    pos = _index(pos, torch.int32, n, dev, "pos")
+    if lse is not None and (lse.dtype != torch.float32 or lse.device != dev or
+                            not lse.is_contiguous() or lse.dim() != 2 or lse.shape[0] < n or
+                            lse.shape[1] != cfg.n_q_heads):
+        raise ValueError(f"lse must be float32 [{n}][{cfg.n_q_heads}], contiguous, on {dev}")
+    with _on(dev):
+        if workspace is None:
+            if stream is not None:
+                raise ValueError("a call on another stream needs a workspace of its own")
+            workspace = cache_attend_workspace(cfg, cache, chunks)
+        elif workspace.device != dev or not workspace.is_contiguous():
+            raise ValueError(f"workspace must be contiguous and lie on {dev}")
+        _check(_lib.c2kv_cache_attend(ctypes.byref(cfg), cache.ref, chunks.ref, qp, qs, pos, op,
+                                      None if lse is None else lse.data_ptr(),
+                                      workspace.data_ptr(),
+                                      workspace.numel() * workspace.element_size(),
+                                      _stream(stream)))
+
+
+def c2kv_pool_write(cfg: AttnCfg, pool: PoolDesc, row, k, v, pos=None, stream=None):
+    """Store the rows k and v [n][H_kv][D] in pool rows row [n] int64, quantised as they are
+    written where the pool is int8; pos [n] int32 encodes k at these positions."""
+    import torch
+    n, dev = int(row.shape[0]), row.device
+    rows = _index(row, torch.int64, n, dev, "row")
+    if not row.is_cuda:
+        raise ValueError("expected a device tensor")
+    if getattr(pool, "row_shape", None) not in (None, (cfg.n_kv_heads, cfg.head_dim)):
+        raise ValueError(f"the pool's rows are {pool.row_shape}, the shape has "
+                         f"{(cfg.n_kv_heads, cfg.head_dim)}")
+    if getattr(pool, "device", dev) != dev:
+        raise ValueError(f"pool on {pool.device}, rows on {dev}")
+    kp, ks = _rows(k, cfg, cfg.n_kv_heads, n, dev, "k")
+    vp, vs = _rows(v, cfg, cfg.n_kv_heads, n, dev, "v")
+    pos = _index(pos, torch.int32, n, dev, "pos")
+    with _on(dev):
+        _check(_lib.c2kv_pool_write(ctypes.byref(cfg), ctypes.byref(pool), n, rows, kp, ks, vp,
+                                    vs, pos, _stream(stream)))
 
 
 class HostPool:

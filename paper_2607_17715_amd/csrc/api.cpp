@@ -3,6 +3,7 @@
 // per-kernel event timing, and the thread-local error text.
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <cstring>
 #include <map>
 #include <mutex>
@@ -12,6 +13,7 @@
 #include <vector>
 
 #include "c2kv.h"
+#include "cache.hpp"
 #include "launch.hpp"
 #include "plan.hpp"
 
@@ -123,6 +125,108 @@ bool check_io(const void* q, const void* ks, const void* vs, const void* out,
     return false;
   }
   return true;
+}
+
+// ---- the growing cache ------------------------------------------------------
+
+// Runs a call's body; nothing thrown in it (a failed host allocation) leaves the C entry.
+template <typename F>
+c2kv_status guarded(F&& body) {
+  try {
+    return body();
+  } catch (...) {
+    g_last_error.clear();
+    return C2KV_E_NOMEM;
+  }
+}
+
+bool on16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+c2kv_status check_shape(const c2kv_attn_cfg* cfg) {
+  if (!cfg) return fail(C2KV_E_INVAL, "cfg is NULL");
+  std::string err;
+  const c2kv_status st = c2kv::check_cfg(*cfg, err);
+  if (st != C2KV_OK) return fail(st, err);
+  if (cfg->n_q_heads > 65535)
+    return fail(C2KV_E_UNSUPPORTED, "more than 65535 query heads are not built");
+  return C2KV_OK;
+}
+
+c2kv_status check_store(const char* what, c2kv_dtype store, const c2kv_attn_cfg& cfg,
+                        const void* k, const void* v, const void* ks, const void* vs) {
+  if (!k || !v) return fail(C2KV_E_INVAL, std::string(what) + "'s K/V pointer is NULL");
+  if (store != C2KV_F32 && store != C2KV_BF16 && store != C2KV_I8)
+    return fail(C2KV_E_INVAL, std::string(what) + " dtype must be F32, BF16 or I8");
+  if ((store == C2KV_F32) != (cfg.act_dtype == C2KV_F32))
+    return fail(C2KV_E_UNSUPPORTED, std::string(what) + "/act dtype combination not built "
+                                                        "(F32/F32, BF16/BF16, I8/BF16)");
+  if (store == C2KV_I8 && (!ks || !vs))
+    return fail(C2KV_E_INVAL, "I8 " + std::string(what) + " needs k_scale and v_scale");
+  if (!on16(k) || !on16(v) || (store == C2KV_I8 && (!on16(ks) || !on16(vs))))
+    return fail(C2KV_E_INVAL, std::string(what) + " memory must lie on 16 bytes");
+  return C2KV_OK;
+}
+
+c2kv_status check_cache(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,
+                        const c2kv_chunks* ch) {
+  c2kv_status st = check_shape(cfg);
+  if (st != C2KV_OK) return st;
+  if (!cache || !ch) return fail(C2KV_E_INVAL, "cache and chunks must not be NULL");
+  st = check_store("cache", cache->dtype, *cfg, cache->k, cache->v, cache->k_scale,
+                   cache->v_scale);
+  if (st != C2KV_OK) return st;
+  if (cache->n_pages < 0) return fail(C2KV_E_INVAL, "n_pages must be >= 0");
+  if (cache->page_size < 1 || cache->page_size % c2kv::kSlotTile != 0)
+    return fail(C2KV_E_INVAL, "page_size must be a positive multiple of " +
+                                  std::to_string(c2kv::kSlotTile) + ", got " +
+                                  std::to_string(cache->page_size));
+  if (cache->page_size > 65536)
+    return fail(C2KV_E_UNSUPPORTED, "pages of more than 65536 tokens are not built");
+  if (ch->batch < 1) return fail(C2KV_E_INVAL, "batch must be >= 1");
+  if (ch->n_tokens < 0 || ch->max_chunk < 0 || ch->max_kv < 0)
+    return fail(C2KV_E_INVAL, "n_tokens, max_chunk and max_kv must be >= 0");
+  if (ch->max_pages < 1) return fail(C2KV_E_INVAL, "max_pages must be >= 1");
+  if (!ch->tok_off || !ch->kv_len || !ch->block_table)
+    return fail(C2KV_E_INVAL, "tok_off, kv_len and block_table must not be NULL");
+  if (int64_t(ch->max_pages) * cache->page_size > (1ll << 30))
+    return fail(C2KV_E_UNSUPPORTED, "block tables of more than 2^30 tokens are not built");
+  if (int64_t(ch->n_tokens) * cfg->n_q_heads > (1ll << 31) - 1 || ch->batch > (1 << 28))
+    return fail(C2KV_E_UNSUPPORTED, "chunks of 2^31 (token, head) rows or more are not built");
+  return C2KV_OK;
+}
+
+// rows of `heads` heads, `stride` elements between tokens (0: dense)
+c2kv_status check_rows(const char* what, const c2kv_attn_cfg& cfg, const void* p, int heads,
+                       int64_t& stride) {
+  if (!p) return fail(C2KV_E_INVAL, std::string(what) + " must not be NULL");
+  const int64_t dense = int64_t(heads) * cfg.head_dim;
+  if (stride == 0) stride = dense;
+  if (stride < dense)
+    return fail(C2KV_E_INVAL, std::string(what) + "'s stride is smaller than a token");
+  if (!on16(p) || stride * (cfg.act_dtype == C2KV_F32 ? 4 : 2) % 16 != 0)
+    return fail(C2KV_E_INVAL, std::string(what) + "'s tokens must lie on 16 bytes");
+  return C2KV_OK;
+}
+
+c2kv::ChunkView view(const c2kv_chunks& c) {
+  return {c.tok_off, c.kv_len, c.block_table, c.batch, c.n_tokens, c.max_pages};
+}
+c2kv::PageView view(const c2kv_cache& c, const c2kv_attn_cfg& cfg) {
+  return {c.k, c.v, c.k_scale, c.v_scale, c.n_pages, c.page_size, cfg.n_kv_heads};
+}
+// theta_i = base^(-2i/D) as turns per position, by powers of the first ratio: 63 products
+// of 64-bit numbers, exact to 1e-14
+c2kv::RopeView rope(const c2kv_attn_cfg& cfg, const int32_t* pos) {
+  c2kv::RopeView r{};
+  r.pos = pos;
+  if (!pos) return r;
+  const double ratio = std::pow(cfg.rope_base, -2.0 / cfg.head_dim);
+  double t = 0.15915494309189533577;          // 1 / (2 pi)
+  for (int i = 0; i < cfg.head_dim / 2; ++i, t *= ratio) r.turns[i] = t;
+  return r;
+}
+int longest_chunk(const c2kv_chunks& c) {
+  return c.max_chunk > 0 && c.max_chunk < c.n_tokens ? c.max_chunk : c.n_tokens;
 }
 
 }  // namespace
@@ -394,6 +498,111 @@ c2kv_status c2kv_load(const c2kv_plan* plan, const c2kv_pool* src, const c2kv_po
     if (e != hipSuccess) return hip_fail(e, "hipMemcpyAsync (load)");
   }
   return C2KV_OK;
+}
+
+c2kv_status c2kv_cache_write(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,
+                             const c2kv_chunks* chunks, const void* k, int64_t k_stride,
+                             const void* v, int64_t v_stride, const int32_t* pos,
+                             void* stream) {
+  return guarded([&] {
+    c2kv_status st = check_cache(cfg, cache, chunks);
+    if (st == C2KV_OK && chunks->n_tokens == 0) return C2KV_OK;
+    if (st == C2KV_OK) st = check_rows("k", *cfg, k, cfg->n_kv_heads, k_stride);
+    if (st == C2KV_OK) st = check_rows("v", *cfg, v, cfg->n_kv_heads, v_stride);
+    if (st != C2KV_OK) return st;
+    const c2kv::WriteParams p{view(*chunks), view(*cache, *cfg), rope(*cfg, pos), k, v,
+                              k_stride, v_stride};
+    hipError_t e = timed("cache_write", [&](hipEvent_t e0, hipEvent_t e1) {
+      return c2kv::launch_cache_write(p, cache->dtype, cfg->head_dim, longest_chunk(*chunks),
+                                      static_cast<hipStream_t>(stream), e0, e1);
+    });
+    return e == hipSuccess ? C2KV_OK : hip_fail(e, "cache write launch");
+  });
+}
+
+c2kv_status c2kv_cache_read(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,
+                            const c2kv_chunks* chunks, const int32_t* turn, void* k, void* v,
+                            void* stream) {
+  return guarded([&] {
+    c2kv_status st = check_cache(cfg, cache, chunks);
+    if (st == C2KV_OK && chunks->n_tokens == 0) return C2KV_OK;
+    int64_t dense = 0;
+    if (st == C2KV_OK) st = check_rows("k", *cfg, k, cfg->n_kv_heads, dense);
+    if (st == C2KV_OK) st = check_rows("v", *cfg, v, cfg->n_kv_heads, dense);
+    if (st != C2KV_OK) return st;
+    const c2kv::ReadParams p{view(*chunks), view(*cache, *cfg), rope(*cfg, turn), k, v};
+    hipError_t e = timed("cache_read", [&](hipEvent_t e0, hipEvent_t e1) {
+      return c2kv::launch_cache_read(p, cache->dtype, cfg->head_dim,
+                                     static_cast<hipStream_t>(stream), e0, e1);
+    });
+    return e == hipSuccess ? C2KV_OK : hip_fail(e, "cache read launch");
+  });
+}
+
+c2kv_status c2kv_cache_attend_workspace(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,
+                                        const c2kv_chunks* chunks, size_t* bytes) {
+  return guarded([&] {
+    const c2kv_status st = check_cache(cfg, cache, chunks);
+    if (st != C2KV_OK) return st;
+    if (!bytes) return fail(C2KV_E_INVAL, "bytes must not be NULL");
+    *bytes = 0;
+    return C2KV_OK;
+  });
+}
+
+c2kv_status c2kv_cache_attend(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,
+                              const c2kv_chunks* chunks, const void* q, int64_t q_stride,
+                              const int32_t* pos, void* out, float* lse, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+  (void)workspace;
+  (void)workspace_bytes;
+  return guarded([&] {
+    c2kv_status st = check_cache(cfg, cache, chunks);
+    if (st == C2KV_OK && chunks->n_tokens == 0) return C2KV_OK;
+    int64_t dense = 0;
+    if (st == C2KV_OK) st = check_rows("q", *cfg, q, cfg->n_q_heads, q_stride);
+    if (st == C2KV_OK) st = check_rows("out", *cfg, out, cfg->n_q_heads, dense);
+    if (st != C2KV_OK) return st;
+    const float scale = cfg->softmax_scale > 0.f ? cfg->softmax_scale
+                                                 : float(1.0 / std::sqrt(double(cfg->head_dim)));
+    const c2kv::AttendParams p{view(*chunks), view(*cache, *cfg), rope(*cfg, pos),
+                               cfg->n_q_heads, cfg->n_q_heads / cfg->n_kv_heads,
+                               float(double(scale) * 1.4426950408889634074), q, q_stride, out,
+                               lse};
+    hipError_t e = timed("cache_attend", [&](hipEvent_t e0, hipEvent_t e1) {
+      return c2kv::launch_cache_attend(p, cache->dtype, cfg->head_dim,
+                                       static_cast<hipStream_t>(stream), e0, e1);
+    });
+    return e == hipSuccess ? C2KV_OK : hip_fail(e, "cache attention launch");
+  });
+}
+
+c2kv_status c2kv_pool_write(const c2kv_attn_cfg* cfg, const c2kv_pool* pool, int32_t n,
+                            const int64_t* row, const void* k, int64_t k_stride,
+                            const void* v, int64_t v_stride, const int32_t* pos,
+                            void* stream) {
+  return guarded([&] {
+    c2kv_status st = check_shape(cfg);
+    if (st != C2KV_OK) return st;
+    if (!pool) return fail(C2KV_E_INVAL, "pool is NULL");
+    st = check_store("pool", pool->dtype, *cfg, pool->k, pool->v, pool->k_scale, pool->v_scale);
+    if (st != C2KV_OK) return st;
+    if (n < 0 || pool->n_rows < 0) return fail(C2KV_E_INVAL, "n and n_rows must be >= 0");
+    if (n == 0) return C2KV_OK;
+    if (!row) return fail(C2KV_E_INVAL, "row must not be NULL");
+    st = check_rows("k", *cfg, k, cfg->n_kv_heads, k_stride);
+    if (st == C2KV_OK) st = check_rows("v", *cfg, v, cfg->n_kv_heads, v_stride);
+    if (st != C2KV_OK) return st;
+    const c2kv::PoolWriteParams p{rope(*cfg, pos), row, n, cfg->n_kv_heads, pool->n_rows, k, v,
+                                  k_stride, v_stride, const_cast<void*>(pool->k),
+                                  const_cast<void*>(pool->v), const_cast<float*>(pool->k_scale),
+                                  const_cast<float*>(pool->v_scale)};
+    hipError_t e = timed("pool_write", [&](hipEvent_t e0, hipEvent_t e1) {
+      return c2kv::launch_pool_write(p, pool->dtype, cfg->head_dim,
+                                     static_cast<hipStream_t>(stream), e0, e1);
+    });
+    return e == hipSuccess ? C2KV_OK : hip_fail(e, "pool write launch");
+  });
 }
 
 c2kv_status c2kv_timing_enable(int32_t on) {

@@ -1,0 +1,666 @@
+// HIP kernels of the growing paged cache for gfx950 (CDNA4).
+//
+//   write_rows_kernel   new tokens into pages, a wavefront per (token, kv-head)
+//   write_tile_kernel   the same for chunks, a workgroup per 64 cache slots
+//   read_tile_kernel    cached tokens back to rows
+//   pool_write_kernel   rows into the chunk pool
+//   attend_kernel       a chunk's queries over its request's pages
+//
+// Lengths, offsets and page numbers are read on the device, so that a captured step
+// can be replayed as they grow.  They are clamped to the buffers that the host named:
+// whatever they hold, nothing outside those is touched.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <type_traits>
+
+#include "cache.hpp"
+#include "cache_index.hpp"
+#include "device.hpp"
+
+namespace c2kv {
+
+namespace {
+
+constexpr int ST = kSlotTile;
+
+// ----------------------------------------------------------------------------
+// requests and their chunks (the index rules are in cache_index.hpp)
+// ----------------------------------------------------------------------------
+
+__device__ inline Req request(const ChunkView& c, int b) {
+  return clamp_req(c.tok_off[b], c.tok_off[b + 1], c.kv_len[b], c.n_tokens);
+}
+
+__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+__device__ inline Req lane_req(const Req& r, int src) {
+  return {uniform(__shfl(r.first, src)), uniform(__shfl(r.n, src)), uniform(__shfl(r.base, src))};
+}
+
+// The request whose chunk holds row `token`, searched by a whole wavefront, 64 requests
+// a step; -1 if none does.
+__device__ inline int find_row(const ChunkView& c, int token, Req& r) {
+  const int lane = threadIdx.x & 63;
+  for (int b0 = 0; b0 < c.batch; b0 += 64) {
+    const int b = b0 + lane;
+    const Req mine = request(c, min(b, c.batch - 1));
+    const uint64_t hit =
+        __ballot(b < c.batch && token >= mine.first && token < mine.first + mine.n);
+    if (hit) {
+      const int src = __builtin_ctzll(hit);
+      r = lane_req(mine, src);
+      return b0 + src;
+    }
+  }
+  return -1;
+}
+
+// Unit u of the batch, where each request has as many units as its chunk has tiles.
+// Searched by a whole wavefront; -1 past the last.
+__device__ inline int find_tile(const ChunkView& c, int limit, int u, Req& r, int& tile) {
+  const int lane = threadIdx.x & 63;
+  int seen = 0;
+  for (int b0 = 0; b0 < c.batch; b0 += 64) {
+    const int b = b0 + lane;
+    const Req mine = request(c, min(b, c.batch - 1));
+    const Tiles t = b < c.batch ? chunk_tiles(mine, limit) : Tiles{0, 0};
+    int incl = t.n;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int x = __shfl_up(incl, d);
+      if (lane >= d) incl += x;
+    }
+    const uint64_t past = __ballot(seen + incl > u);
+    if (past) {
+      const int src = __builtin_ctzll(past);
+      r = lane_req(mine, src);
+      tile = uniform(__shfl(t.t0 + u - (seen + incl - t.n), src));
+      return b0 + src;
+    }
+    seen += uniform(__shfl(incl, 63));
+  }
+  return -1;
+}
+
+// Page of cache index j >= 0 of request b, or -1 where the block table names none.
+__device__ inline int page_of(const ChunkView& c, const PageView& p, int b, int j) {
+  const int col = j / p.PS;
+  if (col >= c.max_pages) return -1;
+  return valid_page(c.table[size_t(b) * c.max_pages + col], p.n_pages);
+}
+
+// ----------------------------------------------------------------------------
+// RoPE and int8
+// ----------------------------------------------------------------------------
+
+// cos and sin of pos positions' turn of a pair: the angle in whole turns is formed and
+// reduced in 64 bits (a far position times a frequency loses its fraction in 32).
+__device__ inline void turn_cs(int pos, double turns, float& c, float& s) {
+  double x = pos * turns;
+  x -= __builtin_rint(x);
+  const float f = float(x);
+  sincospif(2.f * f, &s, &c);
+}
+
+// Largest magnitude as bits, NaN above all: a row that holds one gets a NaN scale, and
+// reads back as NaN.
+__device__ inline uint32_t mag(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+template <int LANES>
+__device__ inline uint32_t lanes_max(uint32_t m) {
+#pragma unroll
+  for (int d = 1; d < LANES; d *= 2) m = max(m, uint32_t(__shfl_xor(int(m), d)));
+  return m;
+}
+
+// Symmetric int8: scale = max / 127 (1 for a row of zeros), code = x / scale to the
+// nearest, ties to even.
+__device__ inline float i8_scale(uint32_t m) {
+  const float s = __uint_as_float(m) / 127.f;
+  return s == 0.f ? 1.f : s;
+}
+__device__ inline int i8_code(float x, float scale) {
+  const float q = __builtin_rintf(x / scale);
+  return q == q ? int(fminf(fmaxf(q, -127.f), 127.f)) : 0;
+}
+__device__ inline uint32_t i8_pack4(const float* x, float scale) {
+  return (i8_code(x[0], scale) & 0xff) | (i8_code(x[1], scale) & 0xff) << 8 |
+         (i8_code(x[2], scale) & 0xff) << 16 | uint32_t(i8_code(x[3], scale)) << 24;
+}
+
+// 8 floats -> 8 consecutive stored elements
+template <typename S>
+__device__ inline void put8(S* p, const float (&x)[8], float scale) {
+  if constexpr (sizeof(S) == 1)
+    *reinterpret_cast<uint2*>(p) = make_uint2(i8_pack4(x, scale), i8_pack4(x + 4, scale));
+  else
+    store8(p, x);
+}
+
+// the word of one element of two neighbouring tokens
+template <typename S> struct PairOf { using type = uint32_t; };
+template <> struct PairOf<float> { using type = float2; };
+template <> struct PairOf<int8_t> { using type = uint16_t; };
+template <typename S>
+__device__ inline typename PairOf<S>::type pair_of(float a, float b, float sa, float sb) {
+  if constexpr (sizeof(S) == 4) return make_float2(a, b);
+  else if constexpr (sizeof(S) == 2) return pack_bf16(a, b);
+  else return uint16_t((i8_code(a, sa) & 0xff) | (i8_code(b, sb) & 0xff) << 8);
+}
+
+// LDS tile of transposed values: D rows of ST tokens, each row's 16-byte blocks permuted
+// by the row / 16, which spreads the columns that a wavefront's rows write over the banks.
+template <typename S, int D>
+struct ValueTile {
+  static constexpr int EPV = 16 / int(sizeof(S));    // tokens per block
+  static constexpr int BLOCKS = ST / EPV;
+  static constexpr int LD = ST + EPV;
+  __device__ static int col(int d, int token) {
+    return token ^ (EPV * ((d >> 4) & (BLOCKS - 1)));
+  }
+};
+
+// ----------------------------------------------------------------------------
+// write
+// ----------------------------------------------------------------------------
+
+// A wavefront per (token, kv-head): lane i holds the key pair (i, i + D/2).  For steps of
+// few tokens a request: bound by latency (two dependent loads: the requests, the page).
+template <typename T, typename S, int D>
+__global__ __launch_bounds__(256) void write_rows_kernel(WriteParams a) {
+  constexpr int VPL = D / 64;                // values per lane
+  const int lane = threadIdx.x & 63;
+  const int unit = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int token = unit / a.pg.Hkv, g = unit % a.pg.Hkv;
+  if (token >= a.ch.n_tokens) return;
+  const T* krow = static_cast<const T*>(a.k) + token * a.k_stride + g * D;
+  const T* vrow = static_cast<const T*>(a.v) + token * a.v_stride + g * D;
+  const int i = lane & (D / 2 - 1);
+  float x = to_f(krow[i]), y = to_f(krow[i + D / 2]);
+  float v[VPL];
+#pragma unroll
+  for (int e = 0; e < VPL; ++e) v[e] = to_f(vrow[lane * VPL + e]);
+  const int pos = a.rope.pos ? a.rope.pos[token] : 0;
+
+  Req r;
+  const int b = find_row(a.ch, token, r);
+  if (b < 0) return;
+  const int j = r.base + token - r.first;
+  if (j < 0) return;
+  const int page = page_of(a.ch, a.pg, b, j);
+  if (page < 0) return;
+  const size_t ph = size_t(page) * a.pg.Hkv + g;
+  const int off = j % a.pg.PS;
+
+  if (a.rope.pos) {
+    float c, s;
+    turn_cs(pos, a.rope.turns[i], c, s);
+    rotate_pair(x, y, c, s);
+  }
+  S* kp = static_cast<S*>(a.pg.k) + (ph * a.pg.PS + off) * D;
+  S* vp = static_cast<S*>(a.pg.v) + ph * D * a.pg.PS + off;
+  if constexpr (sizeof(S) == 1) {
+    uint32_t mv = mag(v[0]);
+#pragma unroll
+    for (int e = 1; e < VPL; ++e) mv = max(mv, mag(v[e]));
+    const float ks = i8_scale(lanes_max<64>(max(mag(x), mag(y))));
+    const float vs = i8_scale(lanes_max<64>(mv));
+    if (lane == 0) {
+      a.pg.k_scale[ph * a.pg.PS + off] = ks;
+      a.pg.v_scale[ph * a.pg.PS + off] = vs;
+    }
+    if (lane < D / 2) {
+      kp[i] = int8_t(i8_code(x, ks));
+      kp[i + D / 2] = int8_t(i8_code(y, ks));
+    }
+#pragma unroll
+    for (int e = 0; e < VPL; ++e)
+      vp[size_t(lane * VPL + e) * a.pg.PS] = int8_t(i8_code(v[e], vs));
+  } else {
+    if (lane < D / 2) {
+      kp[i] = from_f<S>(x);
+      kp[i + D / 2] = from_f<S>(y);
+    }
+#pragma unroll
+    for (int e = 0; e < VPL; ++e) vp[size_t(lane * VPL + e) * a.pg.PS] = from_f<S>(v[e]);
+  }
+}
+
+// A workgroup per 64-slot tile of a request that its chunk touches, for the kv-heads
+// blockIdx.y, blockIdx.y + gridDim.y, ...: keys by rows, values transposed through LDS.
+// The turn of a (token, 8 pairs) unit is formed once for all of a workgroup's heads.
+template <typename T, typename S, int D>
+__global__ __launch_bounds__(256) void write_tile_kernel(WriteParams a) {
+  constexpr int NTH = 256;
+  constexpr int KU = D / 16, NKU = ST * KU / NTH;
+  constexpr int VU = D / 8, NVU = ST / 2 * VU / NTH;
+  using VT = ValueTile<S, D>;
+  __shared__ __attribute__((aligned(16))) S sV[D * VT::LD];
+  const int tid = threadIdx.x, PS = a.pg.PS;
+  Req r;
+  int tile;
+  const int b = find_tile(a.ch, a.ch.max_pages * PS, blockIdx.x, r, tile);
+  if (b < 0) return;
+  const int page = page_of(a.ch, a.pg, b, tile * ST);
+  if (page < 0) return;
+  const int off = tile * ST % PS;
+  const auto [lo, hi, row0] = tile_slots(r, tile);
+
+  float kc[NKU][8], kn[NKU][8];
+  if (a.rope.pos) {
+#pragma unroll
+    for (int i = 0; i < NKU; ++i) {
+      const int u = tid + i * NTH;
+      const int pos = a.rope.pos[row0 + min(max(u / KU, lo), hi - 1)];
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        turn_cs(pos, a.rope.turns[8 * (u % KU) + e], kc[i][e], kn[i][e]);
+    }
+  }
+
+  for (int g = blockIdx.y; g < a.pg.Hkv; g += gridDim.y) {
+    const size_t ph = size_t(page) * a.pg.Hkv + g;
+    S* kp = static_cast<S*>(a.pg.k) + (ph * PS + off) * D;
+    S* vp = static_cast<S*>(a.pg.v) + ph * D * PS + off;
+    float x[NKU][8], y[NKU][8], v[NVU][2][8];
+#pragma unroll
+    for (int i = 0; i < NKU; ++i) {
+      const int u = tid + i * NTH;
+      const T* src = static_cast<const T*>(a.k) + g * D + 8 * (u % KU) +
+                     (row0 + min(max(u / KU, lo), hi - 1)) * a.k_stride;
+      load8(src, x[i]);
+      load8(src + D / 2, y[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < NVU; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int u = tid + i * NTH;
+        load8(static_cast<const T*>(a.v) + g * D + 8 * (u % VU) +
+                  (row0 + min(max(2 * (u / VU) + j, lo), hi - 1)) * a.v_stride,
+              v[i][j]);
+      }
+    // ---- keys
+#pragma unroll
+    for (int i = 0; i < NKU; ++i) {
+      const int u = tid + i * NTH;
+      const int slot = u / KU, c = u % KU;
+      if (a.rope.pos) rotate8(x[i], y[i], kc[i], kn[i]);
+      float scale = 1.f;
+      if constexpr (sizeof(S) == 1) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m = max(m, max(mag(x[i][e]), mag(y[i][e])));
+        scale = i8_scale(lanes_max<KU>(m));
+        if (c == 0 && slot >= lo && slot < hi) a.pg.k_scale[ph * PS + off + slot] = scale;
+      }
+      if (slot >= lo && slot < hi) {
+        put8(kp + slot * D + 8 * c, x[i], scale);
+        put8(kp + slot * D + 8 * c + D / 2, y[i], scale);
+      }
+    }
+    // ---- values: words of two tokens into LDS rows, then rows of 16-byte blocks out
+#pragma unroll
+    for (int i = 0; i < NVU; ++i) {
+      const int u = tid + i * NTH;
+      const int slot = 2 * (u / VU), c = u % VU;
+      float scale[2] = {1.f, 1.f};
+      if constexpr (sizeof(S) == 1) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          uint32_t m = 0;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) m = max(m, mag(v[i][j][e]));
+          scale[j] = i8_scale(lanes_max<VU>(m));
+          if (c == 0 && slot + j >= lo && slot + j < hi)
+            a.pg.v_scale[ph * PS + off + slot + j] = scale[j];
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int d = 8 * c + e;
+        *reinterpret_cast<typename PairOf<S>::type*>(sV + d * VT::LD + VT::col(d, slot)) =
+            pair_of<S>(v[i][0][e], v[i][1][e], scale[0], scale[1]);
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < D * VT::BLOCKS / NTH; ++i) {
+      const int u = tid + i * NTH;
+      const int d = u / VT::BLOCKS, s0 = u % VT::BLOCKS * VT::EPV;
+      const S* from = sV + d * VT::LD + VT::col(d, s0);
+      S* to = vp + size_t(d) * PS + s0;
+      if (s0 >= lo && s0 + VT::EPV <= hi) {
+        *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(from);
+      } else {
+#pragma unroll
+        for (int e = 0; e < VT::EPV; ++e)
+          if (s0 + e >= lo && s0 + e < hi) to[e] = from[e];
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// ----------------------------------------------------------------------------
+// read
+// ----------------------------------------------------------------------------
+
+// The tiles of write_tile_kernel the other way: rows in the activation type, int8 decoded
+// and keys turned in fp32, rounded once.
+template <typename T, typename S, int D>
+__global__ __launch_bounds__(256) void read_tile_kernel(ReadParams a) {
+  constexpr int NTH = 256;
+  constexpr int KU = D / 16, NKU = ST * KU / NTH;
+  constexpr int VU = D / 8, NVU = ST / 2 * VU / NTH;
+  using VT = ValueTile<S, D>;
+  constexpr int NB = D * VT::BLOCKS / NTH;
+  __shared__ __attribute__((aligned(16))) S sV[D * VT::LD];
+  const int tid = threadIdx.x, PS = a.pg.PS;
+  Req r;
+  int tile;
+  const int b = find_tile(a.ch, a.ch.max_pages * PS, blockIdx.x, r, tile);
+  if (b < 0) return;
+  const int page = page_of(a.ch, a.pg, b, tile * ST);
+  if (page < 0) return;
+  const int off = tile * ST % PS;
+  const auto [lo, hi, row0] = tile_slots(r, tile);
+
+  float kc[NKU][8], kn[NKU][8];
+  if (a.rope.pos) {
+#pragma unroll
+    for (int i = 0; i < NKU; ++i) {
+      const int u = tid + i * NTH;
+      const int pos = a.rope.pos[row0 + min(max(u / KU, lo), hi - 1)];
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        turn_cs(pos, a.rope.turns[8 * (u % KU) + e], kc[i][e], kn[i][e]);
+    }
+  }
+
+  for (int g = blockIdx.y; g < a.pg.Hkv; g += gridDim.y) {
+    const size_t ph = size_t(page) * a.pg.Hkv + g;
+    const S* kp = static_cast<const S*>(a.pg.k) + (ph * PS + off) * D;
+    const S* vp = static_cast<const S*>(a.pg.v) + ph * D * PS + off;
+    uint4 blocks[NB];
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      const int u = tid + i * NTH;
+      blocks[i] = *reinterpret_cast<const uint4*>(vp + size_t(u / VT::BLOCKS) * PS +
+                                                  u % VT::BLOCKS * VT::EPV);
+    }
+    float x[NKU][8], y[NKU][8];
+#pragma unroll
+    for (int i = 0; i < NKU; ++i) {
+      const int u = tid + i * NTH;
+      const S* src = kp + (u / KU) * D + 8 * (u % KU);
+      load8(src, x[i]);
+      load8(src + D / 2, y[i]);
+      if constexpr (sizeof(S) == 1) {
+        const float scale = a.pg.k_scale[ph * PS + off + u / KU];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { x[i][e] *= scale; y[i][e] *= scale; }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      const int u = tid + i * NTH;
+      const int d = u / VT::BLOCKS;
+      *reinterpret_cast<uint4*>(sV + d * VT::LD + VT::col(d, u % VT::BLOCKS * VT::EPV)) =
+          blocks[i];
+    }
+#pragma unroll
+    for (int i = 0; i < NKU; ++i) {
+      const int u = tid + i * NTH;
+      const int slot = u / KU;
+      if (a.rope.pos) rotate8(x[i], y[i], kc[i], kn[i]);
+      if (slot >= lo && slot < hi) {
+        T* to = static_cast<T*>(a.k) + (size_t(row0 + slot) * a.pg.Hkv + g) * D + 8 * (u % KU);
+        store8(to, x[i]);
+        store8(to + D / 2, y[i]);
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NVU; ++i) {
+      const int u = tid + i * NTH;
+      const int slot = 2 * (u / VU), c = u % VU;
+      float v[2][8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int d = 8 * c + e;
+        const S* from = sV + d * VT::LD + VT::col(d, slot);
+        if constexpr (sizeof(S) == 1) {
+          v[0][e] = float(from[0]);
+          v[1][e] = float(from[1]);
+        } else {
+          v[0][e] = to_f(from[0]);
+          v[1][e] = to_f(from[1]);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if (slot + j < lo || slot + j >= hi) continue;
+        if constexpr (sizeof(S) == 1) {
+          const float scale = a.pg.v_scale[ph * PS + off + slot + j];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[j][e] *= scale;
+        }
+        store8(static_cast<T*>(a.v) + (size_t(row0 + slot + j) * a.pg.Hkv + g) * D + 8 * c, v[j]);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// ----------------------------------------------------------------------------
+// pool write
+// ----------------------------------------------------------------------------
+
+// A thread per (token, 8 pairs): the unit's keys (and the values of the same columns) for
+// the kv-heads blockIdx.y, blockIdx.y + gridDim.y, ..., its turn formed once for all.
+template <typename T, typename S, int D>
+__global__ __launch_bounds__(256) void pool_write_kernel(PoolWriteParams a) {
+  constexpr int KU = D / 16, TOKENS = 256 / KU;
+  const int c = threadIdx.x % KU;
+  const int64_t token = int64_t(blockIdx.x) * TOKENS + threadIdx.x / KU;
+  const bool in = token < a.n;
+  const int64_t t = in ? token : a.n - 1;
+  const int64_t row = a.row[t];
+  const bool ok = in && row >= 0 && row < a.n_rows;
+  float kc[8], kn[8];
+  if (a.rope.pos) {
+    const int pos = a.rope.pos[t];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) turn_cs(pos, a.rope.turns[8 * c + e], kc[e], kn[e]);
+  }
+  for (int g = blockIdx.y; g < a.Hkv; g += gridDim.y) {
+    float x[2][8], y[2][8];                    // keys, values
+    const T* k = static_cast<const T*>(a.k) + t * a.k_stride + g * D + 8 * c;
+    const T* v = static_cast<const T*>(a.v) + t * a.v_stride + g * D + 8 * c;
+    load8(k, x[0]);
+    load8(k + D / 2, y[0]);
+    load8(v, x[1]);
+    load8(v + D / 2, y[1]);
+    if (a.rope.pos) rotate8(x[0], y[0], kc, kn);
+    float scale[2] = {1.f, 1.f};
+    if constexpr (sizeof(S) == 1) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m = max(m, max(mag(x[j][e]), mag(y[j][e])));
+        scale[j] = i8_scale(lanes_max<KU>(m));
+      }
+    }
+    if (!ok) continue;
+    const size_t rh = size_t(row) * a.Hkv + g;
+    S* pk = static_cast<S*>(a.pool_k) + rh * D + 8 * c;
+    S* pv = static_cast<S*>(a.pool_v) + rh * D + 8 * c;
+    put8(pk, x[0], scale[0]);
+    put8(pk + D / 2, y[0], scale[0]);
+    put8(pv, x[1], scale[1]);
+    put8(pv + D / 2, y[1], scale[1]);
+    if constexpr (sizeof(S) == 1) {
+      if (c == 0) {
+        a.k_scale[rh] = scale[0];
+        a.v_scale[rh] = scale[1];
+      }
+    }
+  }
+}
+
+// ----------------------------------------------------------------------------
+// attend
+// ----------------------------------------------------------------------------
+
+// A wavefront per (token, query head): 64 keys a step, a lane a key for the scores and a
+// column (or two) of the values for the sum.
+template <typename T, typename S, int D>
+__global__ __launch_bounds__(64) void attend_kernel(AttendParams a) {
+  constexpr int VPL = D / 64;
+  __shared__ float sQ[D], sP[ST];
+  const int lane = threadIdx.x, token = blockIdx.x, h = blockIdx.y, g = h / a.G;
+  const int PS = a.pg.PS;
+  Req r;
+  const int b = find_row(a.ch, token, r);
+  if (b < 0) return;
+  if (lane < D / 2) {
+    const T* q = static_cast<const T*>(a.q) + token * a.q_stride + h * D;
+    float x = to_f(q[lane]), y = to_f(q[lane + D / 2]);
+    if (a.rope.pos) {
+      float c, s;
+      turn_cs(a.rope.pos[token], a.rope.turns[lane], c, s);
+      rotate_pair(x, y, c, s);
+    }
+    sQ[lane] = x * a.qscale;
+    sQ[lane + D / 2] = y * a.qscale;
+  }
+  __syncthreads();
+  const int sees = min(r.base + (token - r.first) + 1, a.ch.max_pages * PS);
+  float m = kNegInf, l = 0.f, acc[VPL] = {};
+  for (int k0 = 0; k0 < sees; k0 += ST) {
+    const int page = page_of(a.ch, a.pg, b, k0);
+    if (page < 0) continue;
+    const size_t ph = size_t(page) * a.pg.Hkv + g;
+    const int off = k0 % PS, n = min(ST, sees - k0);
+    const S* kp = static_cast<const S*>(a.pg.k) + (ph * PS + off + min(lane, n - 1)) * D;
+    float s = 0.f;
+    for (int d = 0; d < D; d += 8) {
+      float x[8];
+      load8(kp + d, x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s = __builtin_fmaf(x[e], sQ[d + e], s);
+    }
+    const size_t at = ph * PS + off + min(lane, n - 1);
+    if constexpr (sizeof(S) == 1) s *= a.pg.k_scale[at];
+    if (lane >= n) s = kNegInf;
+    float mt = s;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) mt = fmaxf(mt, __shfl_xor(mt, d));
+    const float m_new = fmaxf(m, mt), ref = m_new == kNegInf ? 0.f : m_new;
+    const float keep = exp2f(m - ref);
+    float p = exp2f(s - ref);
+    l = l * keep + p;
+    m = m_new;
+    if constexpr (sizeof(S) == 1) p *= lane < n ? a.pg.v_scale[at] : 0.f;
+    sP[lane] = p;
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < VPL; ++e) {
+      const S* vp = static_cast<const S*>(a.pg.v) + (ph * D + lane + 64 * e) * PS + off;
+      acc[e] *= keep;
+      for (int j = 0; j < n; ++j) acc[e] = __builtin_fmaf(sP[j], float(vp[j]), acc[e]);
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) l += __shfl_xor(l, d);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  T* out = static_cast<T*>(a.out) + (size_t(token) * a.Hq + h) * D;
+#pragma unroll
+  for (int e = 0; e < VPL; ++e) out[lane + 64 * e] = from_f<T>(acc[e] * inv);
+  if (a.lse && lane == 0)
+    a.lse[size_t(token) * a.Hq + h] = l == 0.f ? kNegInf : (m + log2f(l)) * kLn2;
+}
+
+}  // namespace
+
+// ----------------------------------------------------------------------------
+// launchers
+// ----------------------------------------------------------------------------
+
+namespace {
+
+// Calls f(T, S, D) as tagged types for a cache or pool of type `store`.
+template <typename F>
+hipError_t with_types(int store, int D, F&& f) {
+  auto dim = [&](auto t, auto s) {
+    return D == 64 ? f(t, s, std::integral_constant<int, 64>{})
+                   : f(t, s, std::integral_constant<int, 128>{});
+  };
+  if (store == C2KV_F32) return dim(float{}, float{});
+  if (store == C2KV_BF16) return dim(__bf16{}, __bf16{});
+  return dim(__bf16{}, int8_t{});
+}
+
+// Heads one workgroup runs through: all of them where the tiles alone fill the GPU four
+// times over, fewer where they do not (the turns are then formed again per workgroup).
+int head_groups(int64_t tiles, int heads) {
+  const int64_t want = (4 * 256 + tiles - 1) / (tiles > 0 ? tiles : 1);
+  return int(want < 1 ? 1 : want > heads ? heads : want);
+}
+
+}  // namespace
+
+hipError_t launch_cache_write(const WriteParams& p, int store, int D, int max_chunk,
+                              hipStream_t st, hipEvent_t e0, hipEvent_t e1) {
+  return with_types(store, D, [&](auto t, auto s, auto d) {
+    using T = decltype(t);
+    using S = decltype(s);
+    constexpr int kD = decltype(d)::value;
+    if (max_chunk <= 8) {
+      const int64_t units = int64_t(p.ch.n_tokens) * p.pg.Hkv;
+      return launch(reinterpret_cast<const void*>(&write_rows_kernel<T, S, kD>),
+                    dim3(unsigned((units + 3) / 4)), dim3(256), st, p, e0, e1);
+    }
+    const int64_t tiles = p.ch.n_tokens / ST + 2ll * p.ch.batch;
+    return launch(reinterpret_cast<const void*>(&write_tile_kernel<T, S, kD>),
+                  dim3(unsigned(tiles), head_groups(tiles, p.pg.Hkv)), dim3(256), st, p, e0, e1);
+  });
+}
+
+hipError_t launch_cache_read(const ReadParams& p, int store, int D, hipStream_t st,
+                             hipEvent_t e0, hipEvent_t e1) {
+  return with_types(store, D, [&](auto t, auto s, auto d) {
+    using T = decltype(t);
+    using S = decltype(s);
+    const int64_t tiles = p.ch.n_tokens / ST + 2ll * p.ch.batch;
+    return launch(reinterpret_cast<const void*>(&read_tile_kernel<T, S, decltype(d)::value>),
+                  dim3(unsigned(tiles), head_groups(tiles, p.pg.Hkv)), dim3(256), st, p, e0, e1);
+  });
+}
+
+hipError_t launch_pool_write(const PoolWriteParams& p, int store, int D, hipStream_t st,
+                             hipEvent_t e0, hipEvent_t e1) {
+  return with_types(store, D, [&](auto t, auto s, auto d) {
+    using T = decltype(t);
+    using S = decltype(s);
+    constexpr int kD = decltype(d)::value, kTokens = 256 / (kD / 16);
+    const int64_t blocks = (int64_t(p.n) + kTokens - 1) / kTokens;
+    return launch(reinterpret_cast<const void*>(&pool_write_kernel<T, S, kD>),
+                  dim3(unsigned(blocks), head_groups(blocks, p.Hkv)), dim3(256), st, p, e0, e1);
+  });
+}
+
+hipError_t launch_cache_attend(const AttendParams& p, int store, int D, hipStream_t st,
+                               hipEvent_t e0, hipEvent_t e1) {
+  return with_types(store, D, [&](auto t, auto s, auto d) {
+    using T = decltype(t);
+    using S = decltype(s);
+    return launch(reinterpret_cast<const void*>(&attend_kernel<T, S, decltype(d)::value>),
+                  dim3(unsigned(p.ch.n_tokens), unsigned(p.Hq)), dim3(64), st, p, e0, e1);
+  });
+}
+
+}  // namespace c2kv

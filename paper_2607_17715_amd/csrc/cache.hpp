@@ -1,0 +1,91 @@
+// The growing paged cache: parameters of its kernels and their launchers (defined in
+// cache.hip), called by the C ABI in api.cpp.  Non-null events are stamped at the
+// kernel's start and end.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "c2kv.h"
+#include "cache_index.hpp"
+
+namespace c2kv {
+
+// Chunks of new tokens (c2kv_chunks): device arrays.
+struct ChunkView {
+  const int32_t* tok_off;
+  const int32_t* kv_len;
+  const int32_t* table;
+  int32_t batch, n_tokens, max_pages;
+};
+
+// The cache's pages (c2kv_cache) of one layer.
+struct PageView {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  int32_t n_pages, PS, Hkv;
+};
+
+// RoPE: turns[i] full turns of pair (i, i + D/2) per position, in 64 bits; pos == NULL: no turn.
+struct RopeView {
+  const int32_t* pos;
+  double turns[64];
+};
+
+struct WriteParams {
+  ChunkView ch;
+  PageView pg;
+  RopeView rope;
+  const void* k;
+  const void* v;
+  int64_t k_stride, v_stride;   // elements between tokens
+};
+
+struct ReadParams {
+  ChunkView ch;
+  PageView pg;
+  RopeView rope;
+  void* k;
+  void* v;
+};
+
+struct PoolWriteParams {
+  RopeView rope;
+  const int64_t* row;
+  int32_t n, Hkv;
+  int64_t n_rows;
+  const void* k;
+  const void* v;
+  int64_t k_stride, v_stride;
+  void* pool_k;
+  void* pool_v;
+  float* k_scale;
+  float* v_scale;
+};
+
+struct AttendParams {
+  ChunkView ch;
+  PageView pg;
+  RopeView rope;
+  int32_t Hq, G;
+  float qscale;                 // softmax scale * log2(e)
+  const void* q;
+  int64_t q_stride;
+  void* out;
+  float* lse;                   // [n_tokens][Hq] or NULL
+};
+
+// `store`: type of the cache or pool; its activations are F32 for F32, else BF16.
+hipError_t launch_cache_write(const WriteParams& p, int store, int D, int max_chunk,
+                              hipStream_t st, hipEvent_t e0, hipEvent_t e1);
+hipError_t launch_cache_read(const ReadParams& p, int store, int D, hipStream_t st,
+                             hipEvent_t e0, hipEvent_t e1);
+hipError_t launch_pool_write(const PoolWriteParams& p, int store, int D, hipStream_t st,
+                             hipEvent_t e0, hipEvent_t e1);
+hipError_t launch_cache_attend(const AttendParams& p, int store, int D, hipStream_t st,
+                               hipEvent_t e0, hipEvent_t e1);
+
+}  // namespace c2kv

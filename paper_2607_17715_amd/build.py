@@ -26,7 +26,7 @@ DEVICE_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
           f"--offload-arch={ARCH}", f"-I{INCLUDE}", f"-I{CSRC}"]
 
-SOURCES = ["kernels.hip", "cache.hip", "plan.cpp", "api.cpp"]
+SOURCES = ["kernels.hip", "cache.hip", "attend.hip", "plan.cpp", "api.cpp"]
 
 
 def hipcc() -> str:

@@ -228,6 +228,15 @@ c2kv::RopeView rope(const c2kv_attn_cfg& cfg, const int32_t* pos) {
 int longest_chunk(const c2kv_chunks& c) {
   return c.max_chunk > 0 && c.max_chunk < c.n_tokens ? c.max_chunk : c.n_tokens;
 }
+// Launch shape of an attention call, from the bounds that the host knows.
+c2kv::AttendShape attend_shape(const c2kv_attn_cfg& cfg, const c2kv_cache& cache,
+                               const c2kv_chunks& ch) {
+  const int64_t G = cfg.n_q_heads / cfg.n_kv_heads, longest = longest_chunk(ch);
+  const int64_t room = int64_t(ch.max_pages) * cache.page_size;
+  const int64_t kv = ch.max_kv > 0 && ch.max_kv < room ? ch.max_kv : room;
+  return c2kv::attend_shape(cache.dtype, cfg.head_dim, longest * G, ch.batch,
+                            cfg.n_kv_heads, kv);
+}
 
 }  // namespace
 
@@ -545,7 +554,7 @@ c2kv_status c2kv_cache_attend_workspace(const c2kv_attn_cfg* cfg, const c2kv_cac
     const c2kv_status st = check_cache(cfg, cache, chunks);
     if (st != C2KV_OK) return st;
     if (!bytes) return fail(C2KV_E_INVAL, "bytes must not be NULL");
-    *bytes = 0;
+    *bytes = attend_shape(*cfg, *cache, *chunks).total;
     return C2KV_OK;
   });
 }
@@ -554,8 +563,6 @@ c2kv_status c2kv_cache_attend(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,
                               const c2kv_chunks* chunks, const void* q, int64_t q_stride,
                               const int32_t* pos, void* out, float* lse, void* workspace,
                               size_t workspace_bytes, void* stream) {
-  (void)workspace;
-  (void)workspace_bytes;
   return guarded([&] {
     c2kv_status st = check_cache(cfg, cache, chunks);
     if (st == C2KV_OK && chunks->n_tokens == 0) return C2KV_OK;
@@ -563,17 +570,42 @@ c2kv_status c2kv_cache_attend(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,
     if (st == C2KV_OK) st = check_rows("q", *cfg, q, cfg->n_q_heads, q_stride);
     if (st == C2KV_OK) st = check_rows("out", *cfg, out, cfg->n_q_heads, dense);
     if (st != C2KV_OK) return st;
+    const c2kv::AttendShape sh = attend_shape(*cfg, *cache, *chunks);
+    if (sh.total > 0 && !workspace) return fail(C2KV_E_WORKSPACE, "workspace is NULL");
+    if (reinterpret_cast<uintptr_t>(workspace) % 256 != 0)
+      return fail(C2KV_E_WORKSPACE, "workspace must be 256-byte aligned");
+    if (workspace_bytes < sh.total)
+      return fail(C2KV_E_WORKSPACE, "workspace has " + std::to_string(workspace_bytes) +
+                                        " bytes, the call needs " + std::to_string(sh.total));
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
     const float scale = cfg->softmax_scale > 0.f ? cfg->softmax_scale
                                                  : float(1.0 / std::sqrt(double(cfg->head_dim)));
-    const c2kv::AttendParams p{view(*chunks), view(*cache, *cfg), rope(*cfg, pos),
-                               cfg->n_q_heads, cfg->n_q_heads / cfg->n_kv_heads,
-                               float(double(scale) * 1.4426950408889634074), q, q_stride, out,
-                               lse};
+    c2kv::AttendParams p{};
+    p.ch = view(*chunks);
+    p.pg = view(*cache, *cfg);
+    p.rope = rope(*cfg, pos);
+    p.Hq = cfg->n_q_heads;
+    p.G = cfg->n_q_heads / cfg->n_kv_heads;
+    p.qscale = float(double(scale) * 1.4426950408889634074);
+    p.q = q;
+    p.q_stride = q_stride;
+    p.out = out;
+    p.lse = lse;
+    p.part_o = reinterpret_cast<float*>(ws + sh.part_o);
+    p.part_ml = reinterpret_cast<float2*>(ws + sh.part_ml);
+    p.joins = reinterpret_cast<c2kv::Join*>(ws + sh.joins);
+    const hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e = timed("cache_attend", [&](hipEvent_t e0, hipEvent_t e1) {
-      return c2kv::launch_cache_attend(p, cache->dtype, cfg->head_dim,
-                                       static_cast<hipStream_t>(stream), e0, e1);
+      return c2kv::launch_cache_attend(p, sh, cache->dtype, cfg->head_dim, s, e0, e1);
     });
-    return e == hipSuccess ? C2KV_OK : hip_fail(e, "cache attention launch");
+    if (e != hipSuccess) return hip_fail(e, "cache attention launch");
+    if (sh.groups > 1) {
+      e = timed("cache_merge", [&](hipEvent_t e0, hipEvent_t e1) {
+        return c2kv::launch_cache_merge(p, sh, cache->dtype, cfg->head_dim, s, e0, e1);
+      });
+      if (e != hipSuccess) return hip_fail(e, "cache merge launch");
+    }
+    return C2KV_OK;
   });
 }
 

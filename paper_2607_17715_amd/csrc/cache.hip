@@ -4,7 +4,6 @@
 //   write_tile_kernel   the same for chunks, a workgroup per 64 cache slots
 //   read_tile_kernel    cached tokens back to rows
 //   pool_write_kernel   rows into the chunk pool
-//   attend_kernel       a chunk's queries over its request's pages
 //
 // Lengths, offsets and page numbers are read on the device, so that a captured step
 // can be replayed as they grow.  They are clamped to the buffers that the host named:
@@ -15,46 +14,11 @@
 #include <type_traits>
 
 #include "cache.hpp"
-#include "cache_index.hpp"
-#include "device.hpp"
+#include "cache_device.hpp"
 
 namespace c2kv {
 
 namespace {
-
-constexpr int ST = kSlotTile;
-
-// ----------------------------------------------------------------------------
-// requests and their chunks (the index rules are in cache_index.hpp)
-// ----------------------------------------------------------------------------
-
-__device__ inline Req request(const ChunkView& c, int b) {
-  return clamp_req(c.tok_off[b], c.tok_off[b + 1], c.kv_len[b], c.n_tokens);
-}
-
-__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-
-__device__ inline Req lane_req(const Req& r, int src) {
-  return {uniform(__shfl(r.first, src)), uniform(__shfl(r.n, src)), uniform(__shfl(r.base, src))};
-}
-
-// The request whose chunk holds row `token`, searched by a whole wavefront, 64 requests
-// a step; -1 if none does.
-__device__ inline int find_row(const ChunkView& c, int token, Req& r) {
-  const int lane = threadIdx.x & 63;
-  for (int b0 = 0; b0 < c.batch; b0 += 64) {
-    const int b = b0 + lane;
-    const Req mine = request(c, min(b, c.batch - 1));
-    const uint64_t hit =
-        __ballot(b < c.batch && token >= mine.first && token < mine.first + mine.n);
-    if (hit) {
-      const int src = __builtin_ctzll(hit);
-      r = lane_req(mine, src);
-      return b0 + src;
-    }
-  }
-  return -1;
-}
 
 // Unit u of the batch, where each request has as many units as its chunk has tiles.
 // Searched by a whole wavefront; -1 past the last.
@@ -83,25 +47,9 @@ __device__ inline int find_tile(const ChunkView& c, int limit, int u, Req& r, in
   return -1;
 }
 
-// Page of cache index j >= 0 of request b, or -1 where the block table names none.
-__device__ inline int page_of(const ChunkView& c, const PageView& p, int b, int j) {
-  const int col = j / p.PS;
-  if (col >= c.max_pages) return -1;
-  return valid_page(c.table[size_t(b) * c.max_pages + col], p.n_pages);
-}
-
 // ----------------------------------------------------------------------------
 // RoPE and int8
 // ----------------------------------------------------------------------------
-
-// cos and sin of pos positions' turn of a pair: the angle in whole turns is formed and
-// reduced in 64 bits (a far position times a frequency loses its fraction in 32).
-__device__ inline void turn_cs(int pos, double turns, float& c, float& s) {
-  double x = pos * turns;
-  x -= __builtin_rint(x);
-  const float f = float(x);
-  sincospif(2.f * f, &s, &c);
-}
 
 // Largest magnitude as bits, NaN above all: a row that holds one gets a NaN scale, and
 // reads back as NaN.
@@ -510,80 +458,6 @@ __global__ __launch_bounds__(256) void pool_write_kernel(PoolWriteParams a) {
   }
 }
 
-// ----------------------------------------------------------------------------
-// attend
-// ----------------------------------------------------------------------------
-
-// A wavefront per (token, query head): 64 keys a step, a lane a key for the scores and a
-// column (or two) of the values for the sum.
-template <typename T, typename S, int D>
-__global__ __launch_bounds__(64) void attend_kernel(AttendParams a) {
-  constexpr int VPL = D / 64;
-  __shared__ float sQ[D], sP[ST];
-  const int lane = threadIdx.x, token = blockIdx.x, h = blockIdx.y, g = h / a.G;
-  const int PS = a.pg.PS;
-  Req r;
-  const int b = find_row(a.ch, token, r);
-  if (b < 0) return;
-  if (lane < D / 2) {
-    const T* q = static_cast<const T*>(a.q) + token * a.q_stride + h * D;
-    float x = to_f(q[lane]), y = to_f(q[lane + D / 2]);
-    if (a.rope.pos) {
-      float c, s;
-      turn_cs(a.rope.pos[token], a.rope.turns[lane], c, s);
-      rotate_pair(x, y, c, s);
-    }
-    sQ[lane] = x * a.qscale;
-    sQ[lane + D / 2] = y * a.qscale;
-  }
-  __syncthreads();
-  const int sees = min(r.base + (token - r.first) + 1, a.ch.max_pages * PS);
-  float m = kNegInf, l = 0.f, acc[VPL] = {};
-  for (int k0 = 0; k0 < sees; k0 += ST) {
-    const int page = page_of(a.ch, a.pg, b, k0);
-    if (page < 0) continue;
-    const size_t ph = size_t(page) * a.pg.Hkv + g;
-    const int off = k0 % PS, n = min(ST, sees - k0);
-    const S* kp = static_cast<const S*>(a.pg.k) + (ph * PS + off + min(lane, n - 1)) * D;
-    float s = 0.f;
-    for (int d = 0; d < D; d += 8) {
-      float x[8];
-      load8(kp + d, x);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s = __builtin_fmaf(x[e], sQ[d + e], s);
-    }
-    const size_t at = ph * PS + off + min(lane, n - 1);
-    if constexpr (sizeof(S) == 1) s *= a.pg.k_scale[at];
-    if (lane >= n) s = kNegInf;
-    float mt = s;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) mt = fmaxf(mt, __shfl_xor(mt, d));
-    const float m_new = fmaxf(m, mt), ref = m_new == kNegInf ? 0.f : m_new;
-    const float keep = exp2f(m - ref);
-    float p = exp2f(s - ref);
-    l = l * keep + p;
-    m = m_new;
-    if constexpr (sizeof(S) == 1) p *= lane < n ? a.pg.v_scale[at] : 0.f;
-    sP[lane] = p;
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < VPL; ++e) {
-      const S* vp = static_cast<const S*>(a.pg.v) + (ph * D + lane + 64 * e) * PS + off;
-      acc[e] *= keep;
-      for (int j = 0; j < n; ++j) acc[e] = __builtin_fmaf(sP[j], float(vp[j]), acc[e]);
-    }
-    __syncthreads();
-  }
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) l += __shfl_xor(l, d);
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  T* out = static_cast<T*>(a.out) + (size_t(token) * a.Hq + h) * D;
-#pragma unroll
-  for (int e = 0; e < VPL; ++e) out[lane + 64 * e] = from_f<T>(acc[e] * inv);
-  if (a.lse && lane == 0)
-    a.lse[size_t(token) * a.Hq + h] = l == 0.f ? kNegInf : (m + log2f(l)) * kLn2;
-}
-
 }  // namespace
 
 // ----------------------------------------------------------------------------
@@ -591,18 +465,6 @@ __global__ __launch_bounds__(64) void attend_kernel(AttendParams a) {
 // ----------------------------------------------------------------------------
 
 namespace {
-
-// Calls f(T, S, D) as tagged types for a cache or pool of type `store`.
-template <typename F>
-hipError_t with_types(int store, int D, F&& f) {
-  auto dim = [&](auto t, auto s) {
-    return D == 64 ? f(t, s, std::integral_constant<int, 64>{})
-                   : f(t, s, std::integral_constant<int, 128>{});
-  };
-  if (store == C2KV_F32) return dim(float{}, float{});
-  if (store == C2KV_BF16) return dim(__bf16{}, __bf16{});
-  return dim(__bf16{}, int8_t{});
-}
 
 // Heads one workgroup runs through: all of them where the tiles alone fill the GPU four
 // times over, fewer where they do not (the turns are then formed again per workgroup).
@@ -650,16 +512,6 @@ hipError_t launch_pool_write(const PoolWriteParams& p, int store, int D, hipStre
     const int64_t blocks = (int64_t(p.n) + kTokens - 1) / kTokens;
     return launch(reinterpret_cast<const void*>(&pool_write_kernel<T, S, kD>),
                   dim3(unsigned(blocks), head_groups(blocks, p.Hkv)), dim3(256), st, p, e0, e1);
-  });
-}
-
-hipError_t launch_cache_attend(const AttendParams& p, int store, int D, hipStream_t st,
-                               hipEvent_t e0, hipEvent_t e1) {
-  return with_types(store, D, [&](auto t, auto s, auto d) {
-    using T = decltype(t);
-    using S = decltype(s);
-    return launch(reinterpret_cast<const void*>(&attend_kernel<T, S, decltype(d)::value>),
-                  dim3(unsigned(p.ch.n_tokens), unsigned(p.Hq)), dim3(64), st, p, e0, e1);
   });
 }
 

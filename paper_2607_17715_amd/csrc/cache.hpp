@@ -76,7 +76,29 @@ struct AttendParams {
   int64_t q_stride;
   void* out;
   float* lse;                   // [n_tokens][Hq] or NULL
+  // workspace: what the workgroups of one launch leave for the joining one
+  float* part_o;                // [2 * groups][RB][D]
+  float2* part_ml;              // [2 * groups][RB] reference maximum (base 2), sum
+  struct Join* joins;           // [groups]
 };
+
+// A unit cut by a border between workgroups (joins[w]: the one that begins in workgroup
+// w), nrows 0 where there is none: its pieces are the second partial of workgroup w and
+// the first ones of w + 1 .. last.
+struct Join {
+  int32_t first, row0, nrows, g, last, pad[3];
+};
+
+// How an attention call is launched, and what its workspace holds.
+struct AttendShape {
+  int32_t rows;                 // RB: query rows of a unit
+  int32_t groups;               // workgroups
+  size_t part_o, part_ml, joins, total;   // byte offsets
+};
+// rows_max: bound on the (token, query head) rows of one (request, kv-head), kv_max on a
+// request's cached tokens
+AttendShape attend_shape(int store, int D, int64_t rows_max, int64_t batch, int64_t heads,
+                         int64_t kv_max);
 
 // `store`: type of the cache or pool; its activations are F32 for F32, else BF16.
 hipError_t launch_cache_write(const WriteParams& p, int store, int D, int max_chunk,
@@ -85,7 +107,9 @@ hipError_t launch_cache_read(const ReadParams& p, int store, int D, hipStream_t 
                              hipEvent_t e0, hipEvent_t e1);
 hipError_t launch_pool_write(const PoolWriteParams& p, int store, int D, hipStream_t st,
                              hipEvent_t e0, hipEvent_t e1);
-hipError_t launch_cache_attend(const AttendParams& p, int store, int D, hipStream_t st,
-                               hipEvent_t e0, hipEvent_t e1);
+hipError_t launch_cache_attend(const AttendParams& p, const AttendShape& sh, int store, int D,
+                               hipStream_t st, hipEvent_t e0, hipEvent_t e1);
+hipError_t launch_cache_merge(const AttendParams& p, const AttendShape& sh, int store, int D,
+                              hipStream_t st, hipEvent_t e0, hipEvent_t e1);
 
 }  // namespace c2kv

@@ -18,6 +18,7 @@ constexpr int kSlotTile = 64;   // cache slots of one tile; a page holds whole t
 
 C2KV_INDEX_FN int imin_(int a, int b) { return a < b ? a : b; }
 C2KV_INDEX_FN int imax_(int a, int b) { return a > b ? a : b; }
+C2KV_INDEX_FN int64_t imin64(int64_t a, int64_t b) { return a < b ? a : b; }
 
 // One request's chunk: rows [first, first + n) of the chunk tensors; its row t is cache
 // index base + t (negative where the chunk is longer than the cache's stated length).
@@ -59,6 +60,40 @@ C2KV_INDEX_FN TileSlots tile_slots(const Req& r, int tile) {
 // A block-table entry, or -1 where it names no page.
 C2KV_INDEX_FN int valid_page(int id, int n_pages) {
   return unsigned(id) < unsigned(n_pages) ? id : -1;
+}
+
+// ---- attention work ----------------------------------------------------------------
+//
+// A unit is a block of `rb` query rows of one (request, kv-head); row r of a request's
+// chunk is query head r % G of the kv-head's group at token r / G.  Units are ordered by
+// request, kv-head, row block; a unit's work is its key tiles, and the tiles of all units
+// in that order are one line that the workgroups of a launch share evenly, each a
+// contiguous stretch: whatever the lengths, all finish together.  A unit cut by a border
+// is joined afterwards.
+
+// Keys that exist for row block `i` of a chunk: what its last token sees.
+C2KV_INDEX_FN int unit_keys(const Req& r, int G, int rb, int i, int limit) {
+  const int64_t last = imin64(int64_t(i + 1) * rb, int64_t(r.n) * G) - 1;
+  return int(imin64(imax_(0, r.base + int(last / G) + 1), limit));
+}
+// Its tiles: at least one, so that rows that see no key are answered as well.
+C2KV_INDEX_FN int unit_tiles(const Req& r, int G, int rb, int i, int limit) {
+  return imax_(1, (unit_keys(r, G, rb, i, limit) + kSlotTile - 1) / kSlotTile);
+}
+C2KV_INDEX_FN int row_blocks(const Req& r, int G, int rb) {
+  return int((int64_t(r.n) * G + rb - 1) / rb);
+}
+// Tiles of all row blocks of one kv-head.
+C2KV_INDEX_FN int64_t head_tiles(const Req& r, int G, int rb, int limit) {
+  int64_t t = 0;
+  for (int i = 0, e = row_blocks(r, G, rb); i < e; ++i) t += unit_tiles(r, G, rb, i, limit);
+  return t;
+}
+// First tile of workgroup w's share of `total` tiles, and the workgroup whose share holds
+// tile x (shares of fewer tiles than workgroups are empty for some).
+C2KV_INDEX_FN int64_t share_begin(int64_t total, int W, int w) { return total * w / W; }
+C2KV_INDEX_FN int share_of(int64_t total, int W, int64_t x) {
+  return int(((x + 1) * W - 1) / total);
 }
 
 }  // namespace c2kv

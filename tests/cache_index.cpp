@@ -3,6 +3,7 @@
 // tile in the block-table row, no two units of a well-formed batch share a slot, and the
 // units of a batch are as many as the launches provide for.
 // Usage: cache_index <iterations> <seed>; prints "ok <tiles checked>".
+#include <algorithm>
 #include <cstdio>
 #include <cstdlib>
 #include <limits>
@@ -62,6 +63,46 @@ int main(int argc, char** argv) {
       }
     }
     CHECK(covered == expected);
+    // ---- attention: the shares of all workgroups hold every tile of every unit once, a
+    // unit's pieces lie in consecutive workgroups, and only a workgroup's first piece may
+    // continue a unit and only its last be continued
+    const int G = pick(1, 9), rb = 16 << pick(0, 4), Hkv = pick(1, 3), W = pick(1, 40);
+    int64_t total = 0;
+    std::vector<int64_t> ends;                   // of the units, along the line
+    for (int b = 0; b < B; ++b) {
+      const Req r = clamp_req(off[b], off[b + 1], len[b], n_tokens);
+      CHECK(r.n > 0 || row_blocks(r, G, rb) == 0);
+      for (int g = 0; g < Hkv; ++g)
+        for (int i = 0; i < row_blocks(r, G, rb); ++i) {
+          const int t = unit_tiles(r, G, rb, i, limit), keys = unit_keys(r, G, rb, i, limit);
+          CHECK(t >= 1 && keys >= 0 && keys <= limit && int64_t(t) * kSlotTile >= keys);
+          CHECK(t == 1 || int64_t(t - 1) * kSlotTile < keys);
+          // no row of the block sees more
+          const int last = std::min((i + 1) * rb, r.n * G) - 1;
+          CHECK(keys == std::min(std::max(0, r.base + last / G + 1), limit));
+          total += t;
+          ends.push_back(total);
+        }
+      if (Hkv == 1) CHECK(head_tiles(r, G, rb, limit) ==
+                          (ends.empty() ? 0 : total - [&] {
+                            const int n = row_blocks(r, G, rb);
+                            return int(ends.size()) > n ? ends[ends.size() - n - 1] : int64_t(0);
+                          }()));
+    }
+    if (total > 0) {
+      CHECK(share_begin(total, W, 0) == 0 && share_begin(total, W, W) == total);
+      for (int w = 0; w < W; ++w) {
+        const int64_t p0 = share_begin(total, W, w), p1 = share_begin(total, W, w + 1);
+        CHECK(p0 <= p1);
+        if (p0 == p1) continue;
+        CHECK(share_of(total, W, p0) == w && share_of(total, W, p1 - 1) == w);
+      }
+      for (int64_t e : ends) {
+        const int w = share_of(total, W, e - 1);
+        CHECK(w >= 0 && w < W && share_begin(total, W, w) <= e - 1 &&
+              e - 1 < share_begin(total, W, w + 1));
+      }
+    }
     if (good) CHECK(tiles <= n_tokens / kSlotTile + 2l * B);
   }
   const int it = -1;

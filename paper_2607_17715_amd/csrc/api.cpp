@@ -175,7 +175,7 @@ c2kv_status check_cache(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,
   st = check_store("cache", cache->dtype, *cfg, cache->k, cache->v, cache->k_scale,
                    cache->v_scale);
   if (st != C2KV_OK) return st;
-  if (cache->n_pages < 0) return fail(C2KV_E_INVAL, "n_pages must be >= 0");
+  if (cache->n_pages < 1) return fail(C2KV_E_INVAL, "n_pages must be >= 1");
   if (cache->page_size < 1 || cache->page_size % c2kv::kSlotTile != 0)
     return fail(C2KV_E_INVAL, "page_size must be a positive multiple of " +
                                   std::to_string(c2kv::kSlotTile) + ", got " +

@@ -54,7 +54,8 @@ struct Share {
 };
 
 template <int RB>
-__device__ inline Share find_share(const AttendParams& a, int limit, int least, Place& at) {
+__device__ inline Share find_share(const AttendParams& a, int w, int limit, int least,
+                                   Place& at) {
   const int lane = threadIdx.x & 63;
   Share s{};
   Req mine{};
@@ -70,7 +71,6 @@ __device__ inline Share find_share(const AttendParams& a, int limit, int least, 
   if (s.total == 0) return s;
   const int64_t most = (s.total + least - 1) / least;
   s.groups = int(most < gridDim.x ? most : int64_t(gridDim.x));
-  const int w = blockIdx.x;
   if (w >= s.groups) return s;
   s.p0 = share_begin(s.total, s.groups, w);
   s.p1 = share_begin(s.total, s.groups, w + 1);
@@ -131,24 +131,12 @@ __device__ inline Join cut_unit(const AttendParams& a, const Share& s, const Pla
 // rows
 // ----------------------------------------------------------------------------
 
-// cos and sin of the turns of a unit's tokens, [token - first token][pair]
-template <int RB, int D>
-__device__ inline void unit_turns(const AttendParams& a, const Place& at, int row0, int nrows,
-                                  float2* cs) {
-  const int t0 = row0 / a.G, nt = (row0 + nrows - 1) / a.G - t0 + 1;
-  for (int i = threadIdx.x; i < nt * (D / 2); i += blockDim.x) {
-    float c, s;
-    turn_cs(a.rope.pos[at.r.first + t0 + i / (D / 2)], a.rope.turns[i % (D / 2)], c, s);
-    cs[i] = make_float2(c, s);
-  }
-}
-
-// 8 consecutive elements d0 .. d0 + 7 of a query row, turned and scaled
+// 8 consecutive elements d0 .. d0 + 7 of a query row, turned to pos and scaled
 template <typename T, int D>
-__device__ inline void query8(const T* row, int d0, const float2* cs, float scale,
+__device__ inline void query8(const AttendParams& a, const T* row, int d0, int pos,
                               float (&out)[8]) {
   const int lo = d0 % (D / 2);
-  if (!cs) {
+  if (!a.rope.pos) {
     load8(row + d0, out);
   } else {
     float x[8], y[8];
@@ -156,13 +144,14 @@ __device__ inline void query8(const T* row, int d0, const float2* cs, float scal
     load8(row + lo + D / 2, y);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float2 w = cs[lo + e];
-      rotate_pair(x[e], y[e], w.x, w.y);
+      float c, s;
+      turn_cs(pos, a.rope.turns[lo + e], c, s);
+      rotate_pair(x[e], y[e], c, s);
       out[e] = d0 < D / 2 ? x[e] : y[e];
     }
   }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) out[e] *= scale;
+  for (int e = 0; e < 8; ++e) out[e] *= a.qscale;
 }
 
 __device__ inline bf16x8 bf16_of(const float (&x)[8]) {
@@ -214,14 +203,13 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
 
   __shared__ __attribute__((aligned(16))) float s_o[NW * RB * LDO];
   __shared__ float s_m[NW * RB], s_l[NW * RB];
-  __shared__ float2 s_cs[RB * (D / 2)];
 
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
   const int col = lane & 15, j = lane >> 4;
   const int PS = a.pg.PS, limit = a.ch.max_pages * PS;
   // two tiles a workgroup at least: fewer leave wavefronts without a step
   Place at;
-  const Share share = find_share<RB>(a, limit, I8 ? 4 : 2, at);
+  const Share share = find_share<RB>(a, blockIdx.x, limit, I8 ? 4 : 2, at);
   Join join{};
   int64_t p = share.p0;
 
@@ -284,10 +272,6 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
     for (int k = 0; k < SETS; ++k) fetch(min(s0 + k, max(s1 - 1, s0)), set[k]);
 
     // ---- queries: turned by their tokens' positions, the softmax scale folded in
-    if (a.rope.pos) {
-      unit_turns<RB, D>(a, at, row0, nrows, s_cs);
-      __syncthreads();
-    }
     bf16x8 q[NB][NQC];
     int sees[NB];                            // keys that this lane's rows see
 #pragma unroll
@@ -297,13 +281,12 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
       sees[nb] = min(max(at.r.base + t + 1, 0), limit);
       const T* qrow = static_cast<const T*>(a.q) + (at.r.first + t) * a.q_stride +
                       size_t(at.g * a.G + row % a.G) * D;
-      const float2* cs = a.rope.pos ? s_cs + (t - row0 / a.G) * (D / 2) : nullptr;
+      const int pos = a.rope.pos ? a.rope.pos[at.r.first + t] : 0;
 #pragma unroll
       for (int c = 0; c < NQC; ++c) {
         float x[8];
         // the contraction index follows the keys' 16-byte pieces
-        query8<T, D>(qrow, I8 ? 64 * (c / 2) + 16 * j + 8 * (c % 2) : 32 * c + 8 * j, cs,
-                     a.qscale, x);
+        query8<T, D>(a, qrow, I8 ? 64 * (c / 2) + 16 * j + 8 * (c % 2) : 32 * c + 8 * j, pos, x);
         q[nb][c] = bf16_of(x);
       }
     }
@@ -507,6 +490,370 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
 }
 
 // ----------------------------------------------------------------------------
+// many rows
+// ----------------------------------------------------------------------------
+
+// Tiles of keys and transposed values in LDS, as 16-byte chunks of rows of D (keys) or 64
+// (values) elements; a row's chunks are permuted by its index, so that the operand reads
+// of 32 rows at one column fall on distinct banks without padding.
+template <typename T, int D>
+struct WideTile {
+  static constexpr int EPC = 16 / int(sizeof(T));
+  static constexpr int CK = D / EPC, CV = ST / EPC;        // chunks of a row
+  static constexpr int MK = (CK < 16 ? CK : 16) - 1, MV = (CV < 16 ? CV : 16) - 1;
+  static constexpr int KBYTES = ST * D * int(sizeof(T)), BYTES = 2 * KBYTES;
+  __device__ static int k_at(int key, int ch) { return (key * CK + (ch ^ (key & MK))) * 16; }
+  __device__ static int v_at(int d, int ch) { return KBYTES + (d * CV + (ch ^ (d & MV))) * 16; }
+};
+
+// 64 lanes' 16 bytes each from base + off (per lane) to LDS at `lds` + 16 * lane, in flight
+// until the wavefront's vector-memory count says otherwise (wait_loads).  Written out
+// because the compiler would wait for every such load before any LDS read.
+__device__ inline void load_to_lds(const void* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :: "s"(lds), "v"(off), "s"(base) : "memory");
+}
+// until at most N of this wavefront's loads are in flight, then every wavefront's
+template <int N>
+__device__ inline void wait_loads_barrier() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(N) : "memory");
+}
+__device__ inline void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// 512 threads: RG groups of 32 query rows, and 8 / RG parts of a tile's keys for each.
+// Scores transposed (keys x rows) in 32x32 MFMAs: a lane has one row's scores, for bf16 of
+// 8 consecutive keys at a time (keys are dealt to the MFMA's rows with bits 2 and 3 of
+// their index exchanged), the operand of the P*V product.
+template <typename T, int D, int RG>
+__global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
+  using M = Mma<T>;
+  using W = WideTile<T, D>;
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int SZ = sizeof(T), NTH = 512;
+  constexpr int KG = 8 / RG, NKB = 2 / KG;       // key parts, 32-key blocks of a wavefront
+  static_assert(KG <= 2, "a wavefront has a 32-key block at least");
+  constexpr int RB = 32 * RG;
+  constexpr int NST = F32 ? 2 : 4;               // tiles in LDS
+  constexpr int LK = ST * W::CK / NTH, LV = D * W::CV / NTH, LPT = LK + LV;
+  constexpr int NQC = W::CK / 2;                 // query chunks of a lane (its half's)
+  constexpr int NPC = 16 * NKB / W::EPC;         // probability chunks of a lane
+  constexpr int NDB = D / 32;
+  static_assert(LK >= 1 && LV >= 1 && (NTH / W::CK) % (W::MK + 1) == 0 &&
+                    (NTH / W::CV) % (W::MV + 1) == 0,
+                "a thread's chunks of one tile lie in rows of one permutation");
+
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[NST * W::BYTES];
+  const uint32_t lds0 = uint32_t(uintptr_t((__attribute__((address_space(3))) uint8_t*)lds));
+
+  const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
+  const int col = lane & 31, half = lane >> 5;
+  const int rg = wave % RG, kg = wave / RG;
+  const int PS = a.pg.PS, limit = a.ch.max_pages * PS;
+  // workgroups of one XCD (every eighth) take neighbouring shares, which read the same keys
+  const int nx = gridDim.x / 8;
+  const int w = gridDim.x % 8 == 0 ? int(blockIdx.x % 8) * nx + int(blockIdx.x / 8)
+                                   : int(blockIdx.x);
+  Place at;
+  const Share share = find_share<RB>(a, w, limit, 2, at);
+  Join join{};
+  int64_t p = share.p0;
+
+  // this thread's chunks of a tile: chunk tid + i * 512 of the keys, and of the values
+  const int kkey = tid / W::CK, kch = (tid % W::CK) ^ (kkey & W::MK);
+  const int vrow = tid / W::CV, vch = (tid % W::CV) ^ (vrow & W::MV);
+  const uint32_t kofs = uint32_t(kkey * D * SZ + kch * 16);
+  const uint32_t vofs = uint32_t(vrow * PS * SZ + vch * 16);
+
+  while (p < share.p1) {
+    const int row0 = at.i * RB;
+    const int nrows = int(min(int64_t(RB), int64_t(at.r.n) * a.G - row0));
+    const int t0 = at.tile;
+    const int t1 = int(min(int64_t(at.tiles), t0 + (share.p1 - p)));
+    const int keys = unit_keys(at.r, a.G, RB, at.i, limit);
+    const int32_t* table = a.ch.table + size_t(at.b) * a.ch.max_pages;
+    int ids = -1, ids_from = -(1 << 30);         // pages of tiles ids_from + lane
+
+    auto page_id = [&](int tile) __attribute__((always_inline)) {
+      if (unsigned(tile - ids_from) >= 64u) {
+        ids_from = tile;
+        ids = valid_page(table[min((tile + lane) * ST / PS, a.ch.max_pages - 1)], a.pg.n_pages);
+      }
+      return __builtin_amdgcn_readlane(ids, tile - ids_from);
+    };
+    // a tile without a page is loaded from page 0: its scores are masked, its values zeroed
+    auto load = [&](int tile) __attribute__((always_inline)) {
+      const int page = max(page_id(tile), 0), off = tile * ST % PS;
+      const size_t ph = size_t(page) * a.pg.Hkv + at.g;
+      const T* kp = static_cast<const T*>(a.pg.k) + (ph * PS + off) * D;
+      const T* vp = static_cast<const T*>(a.pg.v) + ph * D * PS + off;
+      const uint32_t to = lds0 + (tile - t0) % NST * W::BYTES + wave * 1024;
+#pragma unroll
+      for (int i = 0; i < LK; ++i)
+        load_to_lds(kp + size_t(i) * (NTH / W::CK) * D, kofs, to + i * NTH * 16);
+#pragma unroll
+      for (int i = 0; i < LV; ++i)
+        load_to_lds(vp + size_t(i) * (NTH / W::CV) * PS, vofs, to + W::KBYTES + i * NTH * 16);
+    };
+
+    // ---- this wavefront's rows
+    const bool rows_here = 32 * rg < nrows;
+    const int row = row0 + min(32 * rg + col, nrows - 1), t = row / a.G;
+    const int sees = min(max(at.r.base + t + 1, 0), limit);
+    // every row's keys, and any row's
+    const int wrow0 = row0 + min(32 * rg, nrows - 1);
+    const int sees_all = min(max(at.r.base + wrow0 / a.G + 1, 0), limit);
+    const int wrow1 = row0 + min(32 * rg + 31, nrows - 1);
+    const int sees_any = min(max(at.r.base + wrow1 / a.G + 1, 0), limit);
+    typename M::Op q[NQC * (F32 ? 4 : 1)];
+    {
+      const T* qrow = static_cast<const T*>(a.q) + (at.r.first + t) * a.q_stride +
+                      size_t(at.g * a.G + row % a.G) * D;
+      const int pos = a.rope.pos ? a.rope.pos[at.r.first + t] : 0;
+      // chunk 2 c + half of the row; its partner D / 2 away is chunk c + NQC / 2's
+#pragma unroll
+      for (int c = 0; c < NQC / 2; ++c) {
+        const int d0 = (2 * c + half) * W::EPC;
+        float x[W::EPC], y[W::EPC];
+#pragma unroll
+        for (int e = 0; e < W::EPC; ++e) {
+          x[e] = to_f(qrow[d0 + e]);
+          y[e] = to_f(qrow[d0 + D / 2 + e]);
+          if (a.rope.pos) {
+            float cc, ss;
+            turn_cs(pos, a.rope.turns[d0 + e], cc, ss);
+            rotate_pair(x[e], y[e], cc, ss);
+          }
+          x[e] *= a.qscale;
+          y[e] *= a.qscale;
+        }
+        if constexpr (F32) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            q[4 * c + e] = x[e];
+            q[4 * (c + NQC / 2) + e] = y[e];
+          }
+        } else {
+          q[c] = bf16_of(x);
+          q[c + NQC / 2] = bf16_of(y);
+        }
+      }
+    }
+
+    // ---- tiles
+#pragma unroll
+    for (int k = 0; k < NST - 1; ++k)
+      if (t0 + k < t1) load(t0 + k);
+
+    float m_run = kNegInf, m_ref = 0.f, l_run = 0.f;
+    f32x16 o[NDB], bias;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) bias[v] = 0.f;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) o[db] = bias;
+
+    auto compute = [&](int tile, int page, const uint8_t* st) __attribute__((always_inline)) {
+      f32x16 s[NKB];
+      // ---- scores (relative to the reference: the chains begin with minus it)
+#pragma unroll
+      for (int b = 0; b < NKB; ++b) {
+        const int kr = 32 * (kg * NKB + b) +
+                       (F32 ? col : (col & ~12) | (col & 4) << 1 | (col & 8) >> 1);
+        s[b] = bias;
+#pragma unroll
+        for (int c = 0; c < NQC; ++c) {
+          const uint8_t* from = st + W::k_at(kr, 2 * c + half);
+          if constexpr (F32) {
+            const float4 f = *reinterpret_cast<const float4*>(from);
+            s[b] = M::run(f.x, q[4 * c], s[b]);
+            s[b] = M::run(f.y, q[4 * c + 1], s[b]);
+            s[b] = M::run(f.z, q[4 * c + 2], s[b]);
+            s[b] = M::run(f.w, q[4 * c + 3], s[b]);
+          } else {
+            s[b] = M::run(*reinterpret_cast<const bf16x8*>(from), q[c], s[b]);
+          }
+        }
+      }
+      // value v of block b is key 32 b + 16 (v / 8) + 8 half + v % 8 (fp32: 8 (v / 4) +
+      // 4 half + v % 4) of the wavefront's part
+      const int k0 = tile * ST + 32 * kg * NKB;
+      if (k0 + 32 * NKB > sees_all || page < 0) {
+        const int lim = page < 0 ? -64 : sees - k0 - (F32 ? 4 : 8) * half - 1;
+#pragma unroll
+        for (int b = 0; b < NKB; ++b)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const int key = 32 * b + (F32 ? 8 * (v >> 2) + (v & 3) : 16 * (v >> 3) + (v & 7));
+            const uint32_t hide = uint32_t((lim - key) >> 31);
+            const uint32_t x = __float_as_uint(s[b][v]);
+            s[b][v] = __uint_as_float((x & ~hide) | (0xff800000u & hide));
+          }
+      }
+      float mx = s[0][0];
+#pragma unroll
+      for (int i = 1; i < 16 * NKB; ++i) mx = fmaxf(mx, s[i / 16][i % 16]);
+      if (__any(mx + m_ref > m_run + kLazyLog2)) {
+        const float m_new = fmaxf(m_run, half_pair_max(mx) + m_ref);
+        const float ref = m_new == kNegInf ? 0.f : m_new;
+        const float keep = __builtin_amdgcn_exp2f(m_run - ref), d = ref - m_ref;
+        l_run *= keep;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) o[db][v] *= keep;
+#pragma unroll
+        for (int b = 0; b < NKB; ++b)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) s[b][v] -= d;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) bias[v] = -ref;
+        m_run = m_new;
+        m_ref = ref;
+      }
+      // ---- probabilities and P*V
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+      if constexpr (F32) {
+#pragma unroll
+        for (int i = 0; i < 16 * NKB; ++i) {
+          const float x = __builtin_amdgcn_exp2f(s[i / 16][i % 16]);
+          s[i / 16][i % 16] = x;
+          sum[i % 4] += x;
+        }
+        // a tile's sum apart, then added: the rounding of a long sum grows with the tiles
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) {
+          f32x16 part;
+#pragma unroll
+          for (int v = 0; v < 16; ++v) part[v] = 0.f;
+#pragma unroll
+          for (int c = 0; c < NPC; ++c) {
+            const float4 f = *reinterpret_cast<const float4*>(
+                st + W::v_at(32 * db + col, 2 * (kg * NPC + c) + half));
+            part = M::run(f.x, s[c / 4][4 * (c % 4)], part);
+            part = M::run(f.y, s[c / 4][4 * (c % 4) + 1], part);
+            part = M::run(f.z, s[c / 4][4 * (c % 4) + 2], part);
+            part = M::run(f.w, s[c / 4][4 * (c % 4) + 3], part);
+          }
+          o[db] += part;
+        }
+      } else {
+        bf16x8 pb[NPC];
+        const bf16x2 ones = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
+#pragma unroll
+        for (int c = 0; c < NPC; ++c)
+#pragma unroll
+          for (int e = 0; e < 8; e += 2) {
+            const f32x2 x = {__builtin_amdgcn_exp2f(s[c / 2][8 * (c % 2) + e]),
+                             __builtin_amdgcn_exp2f(s[c / 2][8 * (c % 2) + e + 1])};
+            const bf16x2 b = __builtin_convertvector(x, bf16x2);
+            pb[c][e] = b[0];
+            pb[c][e + 1] = b[1];
+            // the sum of the rounded values that the product uses
+            sum[e / 2] = __builtin_amdgcn_fdot2_f32_bf16(b, ones, sum[e / 2], false);
+          }
+#pragma unroll
+        for (int c = 0; c < NPC; ++c)
+#pragma unroll
+          for (int db = 0; db < NDB; ++db)
+            o[db] = M::run(*reinterpret_cast<const bf16x8*>(
+                               st + W::v_at(32 * db + col, 2 * (kg * NPC + c) + half)),
+                           pb[c], o[db]);
+      }
+      l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    };
+
+    for (int tile = t0; tile < t1; ++tile) {
+      // this tile's loads are done where only those of the tiles after it are in flight
+      const int after = min(t1 - 1 - tile, NST - 2);
+      if (after >= 2) wait_loads_barrier<2 * LPT>();
+      else if (after == 1) wait_loads_barrier<LPT>();
+      else wait_loads_barrier<0>();
+      // (every wavefront is past the tile before, whose place the next load takes)
+      if (tile + NST - 1 < t1) load(tile + NST - 1);
+      uint8_t* st = lds + (tile - t0) % NST * W::BYTES;
+      const int page = page_id(tile);
+      if ((tile + 1) * ST > keys || page < 0) {
+        // what lies behind the last key may be anything: zero values there
+        const int n = page < 0 ? 0 : max(keys - tile * ST, 0);
+#pragma unroll
+        for (int i = 0; i < LV; ++i) {
+          uint4* v = reinterpret_cast<uint4*>(st + W::KBYTES + (tid + i * NTH) * 16);
+          if (vch * W::EPC + W::EPC > n) *v = keep_first<T>(*v, max(n - vch * W::EPC, 0));
+        }
+        lds_barrier();
+      }
+      if (rows_here && tile * ST < sees_any) compute(tile, page, st);
+    }
+
+    // ---- the key parts of a row group meet
+    float l_tot = half_pair_sum(l_run);
+    if constexpr (KG == 2) {
+      constexpr int XW = 2 + 16 * NDB;
+      static_assert(RG * 64 * XW * 4 <= NST * W::BYTES, "the exchange fits in the stages");
+      lds_barrier();
+      float* mine = reinterpret_cast<float*>(lds) + (rg * 64 + lane) * XW;
+      if (kg == 1) {
+        mine[0] = m_run;
+        mine[1] = l_tot;
+#pragma unroll
+        for (int i = 0; i < 16 * NDB; ++i) mine[2 + i] = o[i / 16][i % 16];
+      }
+      lds_barrier();
+      if (kg == 0) {
+        const float m = fmaxf(m_run, mine[0]), ref = m == kNegInf ? 0.f : m;
+        const float f0 = __builtin_amdgcn_exp2f(m_run - ref);
+        const float f1 = __builtin_amdgcn_exp2f(mine[0] - ref);
+        l_tot = l_tot * f0 + mine[1] * f1;
+        m_run = m;
+#pragma unroll
+        for (int i = 0; i < 16 * NDB; ++i)
+          o[i / 16][i % 16] = o[i / 16][i % 16] * f0 + mine[2 + i] * f1;
+      }
+    }
+    const bool begins = t0 == 0, ends = t1 == at.tiles;
+    if (begins && !ends) join = cut_unit<RB>(a, share, at, t1);
+    if (kg == 0 && 32 * rg + col < nrows) {
+      const float ref = m_run == kNegInf ? 0.f : m_run;
+      // values 4 i .. 4 i + 3 of block db are elements 32 db + 8 i + 4 half + 0 .. 3
+      if (begins && ends) {
+        const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;
+        const size_t oh = size_t(at.r.first + t) * a.Hq + at.g * a.G + row % a.G;
+        T* out = static_cast<T*>(a.out) + oh * D + 4 * half;
+#pragma unroll
+        for (int i = 0; i < 4 * NDB; ++i) {
+          const f32x16& b = o[i / 4];
+          const int v = 4 * (i % 4);
+          if constexpr (F32)
+            *reinterpret_cast<float4*>(out + 8 * i) =
+                make_float4(b[v] * inv, b[v + 1] * inv, b[v + 2] * inv, b[v + 3] * inv);
+          else
+            *reinterpret_cast<uint2*>(out + 8 * i) =
+                make_uint2(pack_bf16(b[v] * inv, b[v + 1] * inv),
+                           pack_bf16(b[v + 2] * inv, b[v + 3] * inv));
+        }
+        if (a.lse && half == 0)
+          a.lse[oh] = l_tot == 0.f ? kNegInf : (ref + __builtin_amdgcn_logf(l_tot)) * kLn2;
+      } else {
+        const size_t part = (size_t(2) * w + (begins ? 1 : 0)) * RB + 32 * rg + col;
+        float* to = a.part_o + part * D + 4 * half;
+#pragma unroll
+        for (int i = 0; i < 4 * NDB; ++i) {
+          const f32x16& b = o[i / 4];
+          const int v = 4 * (i % 4);
+          *reinterpret_cast<float4*>(to + 8 * i) = make_float4(b[v], b[v + 1], b[v + 2], b[v + 3]);
+        }
+        if (half == 0) a.part_ml[part] = make_float2(m_run, l_tot);
+      }
+    }
+    p += t1 - t0;
+    if (p < share.p1) next_unit<RB>(a, limit, at);
+    lds_barrier();                               // LDS of this unit is read
+  }
+  if (tid == 0) a.joins[w] = join;
+}
+
+// ----------------------------------------------------------------------------
 // join
 // ----------------------------------------------------------------------------
 
@@ -570,81 +917,30 @@ __global__ __launch_bounds__(256) void join_kernel(AttendParams a) {
   }
 }
 
-// A wavefront per (token, query head): 64 keys a step, a lane a key for the scores and a
-// column (or two) of the values for the sum.
+template <typename K>
+const void* fn(K* k) { return reinterpret_cast<const void*>(k); }
+
 template <typename T, typename S, int D>
-__global__ __launch_bounds__(64) void attend_token_kernel(AttendParams a) {
-  constexpr int VPL = D / 64;
-  __shared__ float sQ[D], sP[ST];
-  const int lane = threadIdx.x, token = blockIdx.x, h = blockIdx.y, g = h / a.G;
-  const int PS = a.pg.PS;
-  Req r;
-  const int b = find_row(a.ch, token, r);
-  if (b < 0) return;
-  if (lane < D / 2) {
-    const T* q = static_cast<const T*>(a.q) + token * a.q_stride + h * D;
-    float x = to_f(q[lane]), y = to_f(q[lane + D / 2]);
-    if (a.rope.pos) {
-      float c, s;
-      turn_cs(a.rope.pos[token], a.rope.turns[lane], c, s);
-      rotate_pair(x, y, c, s);
-    }
-    sQ[lane] = x * a.qscale;
-    sQ[lane + D / 2] = y * a.qscale;
+const void* attend_fn(int rows) {
+  if constexpr (sizeof(S) == 4) {
+    return fn(&attend_wide_kernel<T, D, 4>);
+  } else {
+    if (rows == 16) return fn(&attend_narrow_kernel<S, D, 1>);
+    if (rows == 32) return fn(&attend_narrow_kernel<S, D, 2>);
+    if constexpr (sizeof(S) == 2)
+      return rows == 128 ? fn(&attend_wide_kernel<T, D, 4>) : fn(&attend_wide_kernel<T, D, 8>);
+    return nullptr;
   }
-  __syncthreads();
-  const int sees = min(r.base + (token - r.first) + 1, a.ch.max_pages * PS);
-  float m = kNegInf, l = 0.f, acc[VPL] = {};
-  for (int k0 = 0; k0 < sees; k0 += ST) {
-    const int page = page_of(a.ch, a.pg, b, k0);
-    if (page < 0) continue;
-    const size_t ph = size_t(page) * a.pg.Hkv + g;
-    const int off = k0 % PS, n = min(ST, sees - k0);
-    const S* kp = static_cast<const S*>(a.pg.k) + (ph * PS + off + min(lane, n - 1)) * D;
-    float s = 0.f;
-    for (int d = 0; d < D; d += 8) {
-      float x[8];
-      load8(kp + d, x);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s = __builtin_fmaf(x[e], sQ[d + e], s);
-    }
-    const size_t at = ph * PS + off + min(lane, n - 1);
-    if constexpr (sizeof(S) == 1) s *= a.pg.k_scale[at];
-    if (lane >= n) s = kNegInf;
-    float mt = s;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) mt = fmaxf(mt, __shfl_xor(mt, d));
-    const float m_new = fmaxf(m, mt), ref = m_new == kNegInf ? 0.f : m_new;
-    const float keep = exp2f(m - ref);
-    float p = exp2f(s - ref);
-    l = l * keep + p;
-    m = m_new;
-    if constexpr (sizeof(S) == 1) p *= lane < n ? a.pg.v_scale[at] : 0.f;
-    sP[lane] = p;
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < VPL; ++e) {
-      const S* vp = static_cast<const S*>(a.pg.v) + (ph * D + lane + 64 * e) * PS + off;
-      acc[e] *= keep;
-      for (int j = 0; j < n; ++j) acc[e] = __builtin_fmaf(sP[j], float(vp[j]), acc[e]);
-    }
-    __syncthreads();
-  }
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) l += __shfl_xor(l, d);
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  T* out = static_cast<T*>(a.out) + (size_t(token) * a.Hq + h) * D;
-#pragma unroll
-  for (int e = 0; e < VPL; ++e) out[lane + 64 * e] = from_f<T>(acc[e] * inv);
-  if (a.lse && lane == 0)
-    a.lse[size_t(token) * a.Hq + h] = l == 0.f ? kNegInf : (m + log2f(l)) * kLn2;
 }
 
-// the kernel of a shape: narrow by rows, else token by token
-template <typename S, int D>
-const void* narrow_kernel(int rows) {
-  return rows == 16 ? reinterpret_cast<const void*>(&attend_narrow_kernel<S, D, 1>)
-                    : reinterpret_cast<const void*>(&attend_narrow_kernel<S, D, 2>);
+template <typename T, int D>
+const void* join_fn(int rows) {
+  if constexpr (sizeof(T) == 4) {
+    return fn(&join_kernel<T, D, 128>);
+  } else {
+    return rows == 16 ? fn(&join_kernel<T, D, 16>) : rows == 32 ? fn(&join_kernel<T, D, 32>)
+         : rows == 128 ? fn(&join_kernel<T, D, 128>) : fn(&join_kernel<T, D, 256>);
+  }
 }
 
 }  // namespace
@@ -653,10 +949,12 @@ AttendShape attend_shape(int store, int D, int64_t rows_max, int64_t batch, int6
                          int64_t kv_max) {
   AttendShape s{};
   auto up = [](size_t x) { return (x + 255) & ~size_t(255); };
-  if (store == C2KV_F32 || rows_max > 32) return s;
-  s.rows = rows_max <= 16 ? 16 : 32;
-  const int64_t tiles = batch * heads * ((kv_max + ST - 1) / ST);
-  s.groups = int(tiles < 512 ? tiles : 512);
+  if (store == C2KV_F32) s.rows = 128;
+  else s.rows = rows_max <= 16 ? 16 : rows_max <= 32 || store == C2KV_I8 ? 32 : rows_max <= 128 ? 128 : 256;
+  const int64_t tiles =
+      batch * heads * ((rows_max + s.rows - 1) / s.rows) * ((kv_max + ST - 1) / ST);
+  const int64_t most = s.rows <= 32 ? 512 : 256;   // two workgroups a CU, or one
+  s.groups = int(tiles < most ? tiles : most);
   size_t at = 0;
   s.part_o = at;
   at = up(at + size_t(2) * s.groups * s.rows * D * sizeof(float));
@@ -669,30 +967,18 @@ AttendShape attend_shape(int store, int D, int64_t rows_max, int64_t batch, int6
 
 hipError_t launch_cache_attend(const AttendParams& p, const AttendShape& sh, int store, int D,
                                hipStream_t st, hipEvent_t e0, hipEvent_t e1) {
-  if (sh.groups > 0) {
-    const void* k = store == C2KV_I8 ? (D == 64 ? narrow_kernel<int8_t, 64>(sh.rows)
-                                                : narrow_kernel<int8_t, 128>(sh.rows))
-                                     : (D == 64 ? narrow_kernel<__bf16, 64>(sh.rows)
-                                                : narrow_kernel<__bf16, 128>(sh.rows));
-    return launch(k, dim3(unsigned(sh.groups)), dim3(256), st, p, e0, e1);
-  }
   return with_types(store, D, [&](auto t, auto s, auto d) {
-    using T = decltype(t);
-    using S = decltype(s);
-    return launch(reinterpret_cast<const void*>(&attend_token_kernel<T, S, decltype(d)::value>),
-                  dim3(unsigned(p.ch.n_tokens), unsigned(p.Hq)), dim3(64), st, p, e0, e1);
+    return launch(attend_fn<decltype(t), decltype(s), decltype(d)::value>(sh.rows),
+                  dim3(unsigned(sh.groups)), dim3(sh.rows <= 32 ? 256 : 512), st, p, e0, e1);
   });
 }
 
 hipError_t launch_cache_merge(const AttendParams& p, const AttendShape& sh, int store, int D,
                               hipStream_t st, hipEvent_t e0, hipEvent_t e1) {
-  (void)store;
-  const void* k =
-      D == 64 ? (sh.rows == 16 ? reinterpret_cast<const void*>(&join_kernel<__bf16, 64, 16>)
-                               : reinterpret_cast<const void*>(&join_kernel<__bf16, 64, 32>))
-              : (sh.rows == 16 ? reinterpret_cast<const void*>(&join_kernel<__bf16, 128, 16>)
-                               : reinterpret_cast<const void*>(&join_kernel<__bf16, 128, 32>));
-  return launch(k, dim3(unsigned(sh.groups), 4), dim3(256), st, p, e0, e1);
+  return with_types(store, D, [&](auto t, auto, auto d) {
+    return launch(join_fn<decltype(t), decltype(d)::value>(sh.rows),
+                  dim3(unsigned(sh.groups), sh.rows <= 32 ? 4 : 32), dim3(256), st, p, e0, e1);
+  });
 }
 
 }  // namespace c2kv

@@ -238,6 +238,14 @@ c2kv::AttendShape attend_shape(const c2kv_attn_cfg& cfg, const c2kv_cache& cache
                             cfg.n_kv_heads, kv);
 }
 
+// Whether the line of key tiles that the device may find passes 32 bits.
+bool too_long(const c2kv::AttendShape& sh, const c2kv_attn_cfg& cfg, const c2kv_cache& cache,
+              const c2kv_chunks& ch) {
+  return c2kv::most_tiles(ch.n_tokens, ch.batch, cfg.n_q_heads / cfg.n_kv_heads, cfg.n_kv_heads,
+                          sh.rows, int64_t(ch.max_pages) * cache.page_size) >= 1ll << 31;
+}
+const char kTooLong[] = "batches that may hold 2^31 key tiles are not built";
+
 }  // namespace
 
 extern "C" {
@@ -554,7 +562,9 @@ c2kv_status c2kv_cache_attend_workspace(const c2kv_attn_cfg* cfg, const c2kv_cac
     const c2kv_status st = check_cache(cfg, cache, chunks);
     if (st != C2KV_OK) return st;
     if (!bytes) return fail(C2KV_E_INVAL, "bytes must not be NULL");
-    *bytes = attend_shape(*cfg, *cache, *chunks).total;
+    const c2kv::AttendShape sh = attend_shape(*cfg, *cache, *chunks);
+    if (too_long(sh, *cfg, *cache, *chunks)) return fail(C2KV_E_UNSUPPORTED, kTooLong);
+    *bytes = sh.total;
     return C2KV_OK;
   });
 }
@@ -571,7 +581,8 @@ c2kv_status c2kv_cache_attend(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,
     if (st == C2KV_OK) st = check_rows("out", *cfg, out, cfg->n_q_heads, dense);
     if (st != C2KV_OK) return st;
     const c2kv::AttendShape sh = attend_shape(*cfg, *cache, *chunks);
-    if (sh.total > 0 && !workspace) return fail(C2KV_E_WORKSPACE, "workspace is NULL");
+    if (too_long(sh, *cfg, *cache, *chunks)) return fail(C2KV_E_UNSUPPORTED, kTooLong);
+    if (!workspace) return fail(C2KV_E_WORKSPACE, "workspace is NULL");
     if (reinterpret_cast<uintptr_t>(workspace) % 256 != 0)
       return fail(C2KV_E_WORKSPACE, "workspace must be 256-byte aligned");
     if (workspace_bytes < sh.total)

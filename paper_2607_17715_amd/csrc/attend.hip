@@ -24,69 +24,75 @@ typedef uint32_t u32x4 __attribute__((__vector_size__(4 * sizeof(uint32_t))));
 // a workgroup's share of the line of tiles
 // ----------------------------------------------------------------------------
 
-template <typename N>
-__device__ inline N wave_scan(N x) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const N y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
-  return x;
+// Inclusive sums over the lanes of a wavefront, by lane moves inside the VALU.  Sums that
+// pass 2^32 stay at its end: lengths and offsets may be anything.
+__device__ inline unsigned add_sat(unsigned x, unsigned y) {
+  return __builtin_elementwise_add_sat(x, y);
 }
-__device__ inline int64_t uniform64(int64_t x) {
-  return int64_t(uint64_t(uint32_t(uniform(int(x >> 32)))) << 32 | uint32_t(uniform(int(x))));
+template <int CTRL, int ROWS>
+__device__ inline unsigned add_from(unsigned x) {
+  return add_sat(x, unsigned(__builtin_amdgcn_update_dpp(0, int(x), CTRL, ROWS, 0xf, false)));
+}
+__device__ inline unsigned wave_scan(unsigned x) {
+  x = add_from<0x111, 0xf>(x);               // from the lane 1, 2, 4, 8 before, in rows of 16
+  x = add_from<0x112, 0xf>(x);
+  x = add_from<0x114, 0xf>(x);
+  x = add_from<0x118, 0xf>(x);
+  x = add_from<0x142, 0xa>(x);               // a row's last lane to the row after it,
+  return add_from<0x143, 0xc>(x);            // and lane 31's to the upper half
 }
 
-// Where a workgroup is on the line: unit (b, g, i) with row block i, the unit's tiles, and
-// the tile at which the workgroup enters it.
+// Where a workgroup is on the line: row block i of (request b, kv-head g), the unit's
+// tiles, and the tile at which the workgroup enters it.
 struct Place {
   Req r;
   int b, g, i, tiles, tile;
 };
 
-// The launch's tiles in all, and the place of the first tile of this workgroup's share
-// [p0, p1); the same in every wavefront.  A share is at least `least` tiles where the line
-// is that long; workgroups past the last share get an empty one.
+// This workgroup's share [p0, p1) of the line and the place of its first tile, the same in
+// every wavefront.  Shares have at least `least` tiles (a power of two) where the line is
+// that long; workgroups past the last get an empty one.
 struct Share {
-  int64_t total, p0, p1;
-  int groups;
+  Shares all;
+  unsigned p0, p1;
 };
 
 template <int RB>
-__device__ inline Share find_share(const AttendParams& a, int w, int limit, int least,
+__device__ inline Share find_share(const AttendParams& a, int w, int limit, unsigned least,
                                    Place& at) {
   const int lane = threadIdx.x & 63;
   Share s{};
   Req mine{};
-  int64_t cost = 0, incl = 0;
+  unsigned head = 0, cost = 0, incl = 0;
   auto step = [&](int b0) {
     const int b = b0 + lane;
     mine = request(a.ch, min(b, a.ch.batch - 1));
-    cost = b < a.ch.batch ? head_tiles(mine, a.G, RB, limit) * a.pg.Hkv : 0;
+    head = b < a.ch.batch ? head_tiles(mine, a.G, RB, limit) : 0;
+    cost = head * a.pg.Hkv;
     incl = wave_scan(cost);
-    return uniform64(__shfl(incl, 63));
+    return unsigned(__builtin_amdgcn_readlane(int(incl), 63));
   };
-  for (int b0 = 0; b0 < a.ch.batch; b0 += 64) s.total += step(b0);
-  if (s.total == 0) return s;
-  const int64_t most = (s.total + least - 1) / least;
-  s.groups = int(most < gridDim.x ? most : int64_t(gridDim.x));
-  if (w >= s.groups) return s;
-  s.p0 = share_begin(s.total, s.groups, w);
-  s.p1 = share_begin(s.total, s.groups, w + 1);
-  int64_t seen = 0;
+  unsigned total = 0;
+  for (int b0 = 0; b0 < a.ch.batch; b0 += 64) total = add_sat(total, step(b0));
+  // (2^31 tiles cannot be where no two requests share a row)
+  if (total == 0 || total >= 1u << 31) return s;
+  s.all = make_shares(total, min((total + least - 1) / least, gridDim.x));
+  if (unsigned(w) >= min((total + least - 1) / least, gridDim.x)) return s;
+  s.p0 = s.all.begin(w);
+  s.p1 = s.all.begin(w + 1);
+  unsigned seen = 0;
   for (int b0 = 0; b0 < a.ch.batch; b0 += 64) {
-    const int64_t here = a.ch.batch > 64 ? step(b0) : s.total;
-    if (s.p0 < seen + here) {
-      const int src = __builtin_ctzll(__ballot(seen + incl > s.p0));
-      at.r = lane_req(mine, src);
+    const unsigned here = a.ch.batch > 64 ? step(b0) : total;
+    if (s.p0 - seen < here) {
+      const int src = __builtin_ctzll(__ballot(incl > s.p0 - seen));
+      auto of = [&](unsigned x) { return unsigned(__builtin_amdgcn_readlane(int(x), src)); };
+      at.r = {int(of(mine.first)), int(of(mine.n)), int(of(mine.base))};
       at.b = b0 + src;
-      int64_t rest = s.p0 - uniform64(__shfl(seen + incl - cost, src));
-      const int64_t per_head = uniform64(__shfl(cost, src)) / a.pg.Hkv;
-      at.g = int(rest / per_head);
-      rest -= at.g * per_head;
+      unsigned rest = s.p0 - seen - (of(incl) - of(cost));
+      at.g = int(rest / of(head));
+      rest -= at.g * of(head);
       at.i = 0;
-      while (rest >= (at.tiles = unit_tiles(at.r, a.G, RB, at.i, limit))) {
+      while (rest >= unsigned(at.tiles = unit_tiles(at.r, a.G, RB, at.i, limit))) {
         rest -= at.tiles;
         ++at.i;
       }
@@ -107,7 +113,8 @@ __device__ inline void next_unit(const AttendParams& a, int limit, Place& at) {
       at.g = 0;
       do {
         ++at.b;
-        at.r = request(a.ch, at.b);
+        const Req r = request(a.ch, at.b);
+        at.r = {uniform(r.first), uniform(r.n), uniform(r.base)};
       } while (at.r.n == 0);
     }
   }
@@ -115,17 +122,29 @@ __device__ inline void next_unit(const AttendParams& a, int limit, Place& at) {
   at.tile = 0;
 }
 
-// The join of the unit that this workgroup's share begins, and ends inside before tile t1.
+// The tiles [t0, t1) of a unit that a workgroup works on.
 template <int RB>
-__device__ inline Join cut_unit(const AttendParams& a, const Share& s, const Place& at, int t1) {
-  Join j{};
-  j.first = at.r.first;
-  j.row0 = at.i * RB;
-  j.nrows = int(min(int64_t(RB), int64_t(at.r.n) * a.G - j.row0));
-  j.g = at.g;
-  j.last = share_of(s.total, s.groups, s.p1 + (at.tiles - t1) - 1);
-  return j;
-}
+struct Piece {
+  Req r;
+  int b, g, t0, t1, tiles, keys, row0, nrows;
+  __device__ Piece(const AttendParams& a, int limit, const Place& at, unsigned left)
+      : r(at.r), b(at.b), g(at.g), t0(at.tile),
+        t1(int(min(unsigned(at.tiles), at.tile + left))), tiles(at.tiles),
+        keys(unit_keys(at.r, a.G, RB, at.i, limit)), row0(at.i * RB),
+        nrows(min(RB, at.r.n * a.G - at.i * RB)) {}
+  __device__ bool begins() const { return t0 == 0; }
+  __device__ bool ends() const { return t1 == tiles; }
+  // the join of a unit that begins in this workgroup, whose share ends (at p1) inside it
+  __device__ Join cut(const Share& s) const {
+    Join j{};
+    j.first = r.first;
+    j.row0 = row0;
+    j.nrows = nrows;
+    j.g = g;
+    j.last = int(s.all.of(s.p1 + unsigned(tiles - t1) - 1));
+    return j;
+  }
+};
 
 // ----------------------------------------------------------------------------
 // rows
@@ -164,6 +183,11 @@ __device__ inline bf16x8 bf16_of_i8(uint32_t w0, uint32_t w1) {
   float x[8];
   raw_to_f8<int8_t>(w, x);
   return bf16_of(x);                       // exact: codes have seven bits
+}
+
+// every wavefront, with its LDS accesses done but its loads still in flight
+__device__ inline void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
 // value of lane k of this lane's group of 16 (a DPP operand of what uses it)
@@ -207,81 +231,90 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
   const int col = lane & 15, j = lane >> 4;
   const int PS = a.pg.PS, limit = a.ch.max_pages * PS;
-  // two tiles a workgroup at least: fewer leave wavefronts without a step
+  // (fewer tiles a workgroup would leave wavefronts without a step)
   Place at;
   const Share share = find_share<RB>(a, blockIdx.x, limit, I8 ? 4 : 2, at);
   Join join{};
-  int64_t p = share.p0;
+  if (share.p0 == share.p1) {
+    if (tid == 0) a.joins[blockIdx.x] = join;
+    return;
+  }
+  unsigned p = share.p0;
+  Piece<RB> cur(a, limit, at, share.p1 - p);
 
-  while (p < share.p1) {
-    const int row0 = at.i * RB;
-    const int nrows = int(min(int64_t(RB), int64_t(at.r.n) * a.G - row0));
-    const int t0 = at.tile;
-    const int t1 = int(min(int64_t(at.tiles), t0 + (share.p1 - p)));
-    const int keys = unit_keys(at.r, a.G, RB, at.i, limit);
+  // ---- loads of this wavefront's steps [s0, s1) of the current piece
+  struct Set {
+    u32x4 k[NKF], v[NVF];
+    float ks, vs;
+    int page;
+  } set[SETS];
+  int s0 = 0, s1 = 0;
+  int ids = -1, ids_from = 0;                // pages of tiles ids_from + lane
+  const int kofs = (8 * U * (col >> 2) + (col & 3)) * D * SZ + 16 * j;
+  const int vofs = col * PS * SZ + 16 * j;
+  auto fetch_ids = [&](int tile) __attribute__((always_inline)) {
+    ids_from = tile;
+    ids = valid_page(a.ch.table[size_t(cur.b) * a.ch.max_pages +
+                                min(int(unsigned((tile + lane) * ST) / unsigned(PS)),
+                                    a.ch.max_pages - 1)],
+                     a.pg.n_pages);
+  };
+  auto fetch = [&](int step, Set& x) __attribute__((always_inline)) {
+    const int tile = step / SPT;
+    if (tile - ids_from >= 64) fetch_ids(tile);
+    x.page = __builtin_amdgcn_readlane(ids, tile - ids_from);
+    // past the last step, and where there is no page: descriptors without extent, whose
+    // loads give zeros and touch no memory
+    const bool real = step < s1 && x.page >= 0;
+    const size_t ph = size_t(real ? x.page : 0) * a.pg.Hkv + cur.g;
+    const int off = unsigned(step * KS) % unsigned(PS);
+    const __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(
+        static_cast<S*>(a.pg.k) + (ph * PS + off) * D, 0, real ? KS * D * SZ : 0, kBufferFlags);
+    const __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(
+        static_cast<S*>(a.pg.v) + ph * D * PS + off, 0, real ? ((D - 1) * PS + KS) * SZ : 0,
+        kBufferFlags);
+#pragma unroll
+    for (int m = 0; m < 2 * U; ++m)
+#pragma unroll
+      for (int c = 0; c < NKC; ++c)
+        x.k[m * NKC + c] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+            kr, kofs + 4 * m * D * SZ + 64 * c, 0, 0));
+#pragma unroll
+    for (int db = 0; db < NVF; ++db)
+      x.v[db] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+          vr, vofs + 16 * db * PS * SZ, 0, 0));
+    if constexpr (I8) {
+      const __amdgpu_buffer_rsrc_t ksr = __builtin_amdgcn_make_buffer_rsrc(
+          a.pg.k_scale + ph * PS + off, 0, real ? KS * 4 : 0, kBufferFlags);
+      const __amdgpu_buffer_rsrc_t vsr = __builtin_amdgcn_make_buffer_rsrc(
+          a.pg.v_scale + ph * PS + off, 0, real ? KS * 4 : 0, kBufferFlags);
+      x.ks = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(ksr, 4 * lane, 0, 0));
+      x.vs = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(vsr, 4 * lane, 0, 0));
+    }
+  };
+  // a piece's first steps
+  auto enter = [&]() __attribute__((always_inline)) {
+    const int n = (cur.t1 - cur.t0) * SPT;
+    s0 = cur.t0 * SPT + n * wave / NW;
+    s1 = cur.t0 * SPT + n * (wave + 1) / NW;
+    fetch_ids(s0 / SPT);
+#pragma unroll
+    for (int k = 0; k < SETS; ++k) fetch(s0 + k, set[k]);
+  };
+  enter();
 
-    // ---- this wavefront's steps and their loads
-    const int n_steps = (t1 - t0) * SPT;
-    const int s0 = t0 * SPT + n_steps * wave / NW, s1 = t0 * SPT + n_steps * (wave + 1) / NW;
-    const int32_t* table = a.ch.table + size_t(at.b) * a.ch.max_pages;
-    int ids = -1, ids_from = -(1 << 30);     // pages of tiles ids_from + lane
-    struct Set {
-      u32x4 k[NKF], v[NVF];
-      float ks, vs;
-      int page;
-    } set[SETS];
-    auto fetch = [&](int step, Set& x) __attribute__((always_inline)) {
-      const int tile = step / SPT;
-      if (unsigned(tile - ids_from) >= 64u) {
-        ids_from = tile;
-        const int c = (tile + lane) * ST / PS;
-        ids = valid_page(table[min(c, a.ch.max_pages - 1)], a.pg.n_pages);
-      }
-      x.page = __builtin_amdgcn_readlane(ids, tile - ids_from);
-      // past the last step, and where there is no page: descriptors without extent, whose
-      // loads give zeros and touch no memory
-      const bool real = step < s1 && x.page >= 0;
-      const size_t ph = size_t(real ? x.page : 0) * a.pg.Hkv + at.g;
-      const int off = (step * KS) % PS;
-      const __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(
-          static_cast<S*>(a.pg.k) + (ph * PS + off) * D, 0, real ? KS * D * SZ : 0, kBufferFlags);
-      const __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(
-          static_cast<S*>(a.pg.v) + ph * D * PS + off, 0,
-          real ? ((D - 1) * PS + KS) * SZ : 0, kBufferFlags);
-      const int kofs = (8 * U * (col >> 2) + (col & 3)) * D * SZ + 16 * j;
-#pragma unroll
-      for (int m = 0; m < 2 * U; ++m)
-#pragma unroll
-        for (int c = 0; c < NKC; ++c)
-          x.k[m * NKC + c] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
-              kr, kofs + 4 * m * D * SZ + 64 * c, 0, 0));
-#pragma unroll
-      for (int db = 0; db < NVF; ++db)
-        x.v[db] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
-            vr, (16 * db + col) * PS * SZ + 16 * j, 0, 0));
-      if constexpr (I8) {
-        const __amdgpu_buffer_rsrc_t ksr = __builtin_amdgcn_make_buffer_rsrc(
-            a.pg.k_scale + ph * PS + off, 0, real ? KS * 4 : 0, kBufferFlags);
-        const __amdgpu_buffer_rsrc_t vsr = __builtin_amdgcn_make_buffer_rsrc(
-            a.pg.v_scale + ph * PS + off, 0, real ? KS * 4 : 0, kBufferFlags);
-        x.ks = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(ksr, 4 * lane, 0, 0));
-        x.vs = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(vsr, 4 * lane, 0, 0));
-      }
-    };
-#pragma unroll
-    for (int k = 0; k < SETS; ++k) fetch(min(s0 + k, max(s1 - 1, s0)), set[k]);
-
+  while (true) {
     // ---- queries: turned by their tokens' positions, the softmax scale folded in
     bf16x8 q[NB][NQC];
     int sees[NB];                            // keys that this lane's rows see
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      const int row = row0 + min(16 * nb + col, nrows - 1);
-      const int t = row / a.G;
-      sees[nb] = min(max(at.r.base + t + 1, 0), limit);
-      const T* qrow = static_cast<const T*>(a.q) + (at.r.first + t) * a.q_stride +
-                      size_t(at.g * a.G + row % a.G) * D;
-      const int pos = a.rope.pos ? a.rope.pos[at.r.first + t] : 0;
+      const unsigned row = cur.row0 + min(16 * nb + col, cur.nrows - 1);
+      const int t = row / unsigned(a.G);
+      sees[nb] = min(max(cur.r.base + t + 1, 0), limit);
+      const T* qrow = static_cast<const T*>(a.q) + (cur.r.first + t) * a.q_stride +
+                      size_t(cur.g * a.G + row - t * a.G) * D;
+      const int pos = a.rope.pos ? a.rope.pos[cur.r.first + t] : 0;
 #pragma unroll
       for (int c = 0; c < NQC; ++c) {
         float x[8];
@@ -290,7 +323,9 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
         q[nb][c] = bf16_of(x);
       }
     }
-    const int sees_all = min(max(at.r.base + row0 / a.G + 1, 0), limit);   // every row's keys
+    const int sees_all = min(max(cur.r.base + int(unsigned(cur.row0) / unsigned(a.G)) + 1, 0),
+                             limit);         // every row's keys
+    const int keys = cur.keys;
 
     float m_run[NB], m_ref[NB], l_run[NB];
     f32x4 o[NB][NVF];
@@ -427,7 +462,17 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
       }
     }
 
-    // ---- the wavefronts' pieces meet
+    // ---- the next piece's first loads, under the end of this one
+    const Piece<RB> old = cur;
+    p += old.t1 - old.t0;
+    const bool more = p < share.p1;
+    if (more) {
+      next_unit<RB>(a, limit, at);
+      cur = Piece<RB>(a, limit, at, share.p1 - p);
+      enter();
+    }
+
+    // ---- the wavefronts' parts meet
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       float l = l_run[nb];
@@ -442,12 +487,11 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
       for (int db = 0; db < NVF; ++db)
         *reinterpret_cast<f32x4*>(s_o + r * LDO + 16 * db + 4 * j) = o[nb][db];
     }
-    __syncthreads();
-    const bool begins = t0 == 0, ends = t1 == at.tiles;
-    if (begins && !ends) join = cut_unit<RB>(a, share, at, t1);
+    lds_barrier();
+    if (old.begins() && !old.ends()) join = old.cut(share);
     constexpr int TPR = 256 / RB, EPT = D / TPR;    // threads a row, elements a thread
     const int row = tid / TPR, d0 = tid % TPR * EPT;
-    if (row < nrows) {
+    if (row < old.nrows) {
       float m = kNegInf, l = 0.f, x[EPT] = {};
 #pragma unroll
       for (int w = 0; w < NW; ++w) m = fmaxf(m, s_m[w * RB + row]);
@@ -459,20 +503,20 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
 #pragma unroll
         for (int e = 0; e < EPT; ++e) x[e] += f * s_o[(w * RB + row) * LDO + d0 + e];
       }
-      if (begins && ends) {
-        const int r = row0 + row, token = at.r.first + r / a.G, h = at.g * a.G + r % a.G;
+      if (old.begins() && old.ends()) {
+        const unsigned r = old.row0 + row, t = r / unsigned(a.G);
+        const size_t oh = size_t(old.r.first + t) * a.Hq + old.g * a.G + (r - t * a.G);
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        T* out = static_cast<T*>(a.out) + (size_t(token) * a.Hq + h) * D + d0;
+        T* out = static_cast<T*>(a.out) + oh * D + d0;
 #pragma unroll
         for (int e = 0; e < EPT; e += 4)
           *reinterpret_cast<uint2*>(out + e) =
               make_uint2(pack_bf16(x[e] * inv, x[e + 1] * inv),
                          pack_bf16(x[e + 2] * inv, x[e + 3] * inv));
         if (a.lse && d0 == 0)
-          a.lse[size_t(token) * a.Hq + h] =
-              l == 0.f ? kNegInf : (ref + __builtin_amdgcn_logf(l)) * kLn2;
+          a.lse[oh] = l == 0.f ? kNegInf : (ref + __builtin_amdgcn_logf(l)) * kLn2;
       } else {
-        const size_t part = (size_t(2) * blockIdx.x + (begins ? 1 : 0)) * RB + row;
+        const size_t part = (size_t(2) * blockIdx.x + (old.begins() ? 1 : 0)) * RB + row;
 #pragma unroll
         for (int e = 0; e < EPT; e += 4)
           *reinterpret_cast<float4*>(a.part_o + part * D + d0 + e) =
@@ -480,11 +524,8 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
         if (d0 == 0) a.part_ml[part] = make_float2(m, l);
       }
     }
-    p += t1 - t0;
-    if (p < share.p1) {
-      next_unit<RB>(a, limit, at);
-      __syncthreads();                       // LDS of this unit is read
-    }
+    if (!more) break;
+    lds_barrier();                           // LDS of this piece is read
   }
   if (tid == 0) a.joins[blockIdx.x] = join;
 }
@@ -517,9 +558,6 @@ __device__ inline void load_to_lds(const void* base, uint32_t off, uint32_t lds)
 template <int N>
 __device__ inline void wait_loads_barrier() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(N) : "memory");
-}
-__device__ inline void lds_barrier() {
-  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
 // 512 threads: RG groups of 32 query rows, and 8 / RG parts of a tile's keys for each.
@@ -558,7 +596,7 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
   Place at;
   const Share share = find_share<RB>(a, w, limit, 2, at);
   Join join{};
-  int64_t p = share.p0;
+  unsigned p = share.p0;
 
   // this thread's chunks of a tile: chunk tid + i * 512 of the keys, and of the values
   const int kkey = tid / W::CK, kch = (tid % W::CK) ^ (kkey & W::MK);
@@ -567,11 +605,8 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
   const uint32_t vofs = uint32_t(vrow * PS * SZ + vch * 16);
 
   while (p < share.p1) {
-    const int row0 = at.i * RB;
-    const int nrows = int(min(int64_t(RB), int64_t(at.r.n) * a.G - row0));
-    const int t0 = at.tile;
-    const int t1 = int(min(int64_t(at.tiles), t0 + (share.p1 - p)));
-    const int keys = unit_keys(at.r, a.G, RB, at.i, limit);
+    const Piece<RB> cur(a, limit, at, share.p1 - p);
+    const int t0 = cur.t0, t1 = cur.t1, row0 = cur.row0, nrows = cur.nrows, keys = cur.keys;
     const int32_t* table = a.ch.table + size_t(at.b) * a.ch.max_pages;
     int ids = -1, ids_from = -(1 << 30);         // pages of tiles ids_from + lane
 
@@ -596,6 +631,11 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
       for (int i = 0; i < LV; ++i)
         load_to_lds(vp + size_t(i) * (NTH / W::CV) * PS, vofs, to + W::KBYTES + i * NTH * 16);
     };
+
+    // ---- the first tiles
+#pragma unroll
+    for (int k = 0; k < NST - 1; ++k)
+      if (t0 + k < t1) load(t0 + k);
 
     // ---- this wavefront's rows
     const bool rows_here = 32 * rg < nrows;
@@ -640,11 +680,6 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
         }
       }
     }
-
-    // ---- tiles
-#pragma unroll
-    for (int k = 0; k < NST - 1; ++k)
-      if (t0 + k < t1) load(t0 + k);
 
     float m_run = kNegInf, m_ref = 0.f, l_run = 0.f;
     f32x16 o[NDB], bias;
@@ -811,8 +846,8 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
           o[i / 16][i % 16] = o[i / 16][i % 16] * f0 + mine[2 + i] * f1;
       }
     }
-    const bool begins = t0 == 0, ends = t1 == at.tiles;
-    if (begins && !ends) join = cut_unit<RB>(a, share, at, t1);
+    const bool begins = cur.begins(), ends = cur.ends();
+    if (begins && !ends) join = cur.cut(share);
     if (kg == 0 && 32 * rg + col < nrows) {
       const float ref = m_run == kNegInf ? 0.f : m_run;
       // values 4 i .. 4 i + 3 of block db are elements 32 db + 8 i + 4 half + 0 .. 3
@@ -857,63 +892,80 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
 // join
 // ----------------------------------------------------------------------------
 
-// Rows blockIdx.y, blockIdx.y + gridDim.y, ... of the unit that workgroup blockIdx.x began
-// and others finished: the four wavefronts take every fourth piece, a lane two columns.
-template <typename T, int D, int RB>
+// The unit that workgroup blockIdx.x began and others finished.  Its rows are dealt to the
+// NW / PW sets of PW wavefronts of all the workgroups blockIdx.y; a set's wavefronts take
+// every PW-th piece, a lane D / 64 columns.  Bound by two dependent loads (the join, the
+// pieces) and the partials' bytes: units of few rows have many pieces (PW = 4), large ones
+// few (PW = 1).
+template <typename T, int D, int RB, int PW>
 __global__ __launch_bounds__(256) void join_kernel(AttendParams a) {
-  constexpr int CPL = D / 64;                // columns of a lane
-  __shared__ float s_x[4][D];
-  const int w0 = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  constexpr int CPL = D / 64, NW = 4, N = 8; // columns of a lane; pieces in flight
+  __shared__ float s_x[NW][D];
+  const int w0 = blockIdx.x, wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const Join jn = a.joins[w0];
   const int pieces = jn.last - w0 + 1;
   // piece k: the second partial of w0, then the first ones of those after it
-  auto slot = [&](int k) { return size_t(2) * (w0 + k) + (k == 0 ? 1 : 0); };
-  for (int row = blockIdx.y; row < jn.nrows; row += gridDim.y) {
-    float m = kNegInf;
-    for (int k = lane; k < pieces; k += 64) m = fmaxf(m, a.part_ml[slot(k) * RB + row].x);
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
-    const float ref = m == kNegInf ? 0.f : m;
-    float l = 0.f;
-    for (int k = lane; k < pieces; k += 64) {
-      const float2 ml = a.part_ml[slot(k) * RB + row];
-      l += ml.y * __builtin_amdgcn_exp2f(ml.x - ref);
-    }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) l += __shfl_xor(l, d);
-    float x[CPL] = {};
-    constexpr int N = 8;
-    for (int k0 = wave; k0 < pieces; k0 += 4 * N) {
-      float v[N][CPL], f[N];
+  auto at = [&](int k, int row) { return (size_t(2) * (w0 + k) + (k == 0 ? 1 : 0)) * RB + row; };
+  const int mine = wave % PW;
+  for (int row = blockIdx.y * (NW / PW) + wave / PW; row < jn.nrows;
+       row += gridDim.y * (NW / PW)) {
+    float x[CPL] = {}, m = kNegInf, l = 0.f;
+    for (int k0 = 0; k0 < pieces; k0 += PW * N) {
+      float v[N][CPL];
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int k = min(k0 + 4 * i, pieces - 1);
-        const float* o = a.part_o + (slot(k) * RB + row) * D + lane * CPL;
+        const float* o = a.part_o + at(min(k0 + PW * i + mine, pieces - 1), row) * D + lane * CPL;
 #pragma unroll
         for (int e = 0; e < CPL; ++e) v[i][e] = o[e];
-        f[i] = a.part_ml[slot(k) * RB + row].x;
       }
+      // lane k has the maximum and the sum of piece k0 + k
+      float2 ml = make_float2(kNegInf, 0.f);
+      if (lane < PW * N && k0 + lane < pieces) ml = a.part_ml[at(k0 + lane, row)];
+      float m_new = ml.x;
+#pragma unroll
+      for (int d = 1; d < PW * N; d *= 2) m_new = fmaxf(m_new, __shfl_xor(m_new, d));
+      m_new = fmaxf(m, __shfl(m_new, 0));
+      const float ref = m_new == kNegInf ? 0.f : m_new;
+      const float keep = __builtin_amdgcn_exp2f(m - ref);
+      const float f = __builtin_amdgcn_exp2f(ml.x - ref);
+      float sum = f * ml.y;
+#pragma unroll
+      for (int d = 1; d < PW * N; d *= 2) sum += __shfl_xor(sum, d);
+      l = l * keep + __shfl(sum, 0);
+      m = m_new;
+#pragma unroll
+      for (int e = 0; e < CPL; ++e) x[e] *= keep;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        if (k0 + 4 * i >= pieces) continue;
-        const float g = __builtin_amdgcn_exp2f(f[i] - ref);
+        if (k0 + PW * i + mine >= pieces) continue;
+        const float g = __shfl(f, PW * i + mine);
 #pragma unroll
         for (int e = 0; e < CPL; ++e) x[e] = __builtin_fmaf(g, v[i][e], x[e]);
       }
     }
+    if constexpr (PW > 1) {
+      static_assert(PW == NW, "one row a workgroup and turn");
 #pragma unroll
-    for (int e = 0; e < CPL; ++e) s_x[wave][lane * CPL + e] = x[e];
-    __syncthreads();
-    if (tid < D) {
-      const int r = jn.row0 + row, token = jn.first + r / a.G, h = jn.g * a.G + r % a.G;
-      const float sum = (s_x[0][tid] + s_x[1][tid]) + (s_x[2][tid] + s_x[3][tid]);
-      static_cast<T*>(a.out)[(size_t(token) * a.Hq + h) * D + tid] =
-          from_f<T>(l == 0.f ? 0.f : sum / l);
-      if (a.lse && tid == 0)
-        a.lse[size_t(token) * a.Hq + h] =
-            l == 0.f ? kNegInf : (ref + __builtin_amdgcn_logf(l)) * kLn2;
+      for (int e = 0; e < CPL; ++e) s_x[wave][lane * CPL + e] = x[e];
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < CPL; ++e) {
+        const int d = lane * CPL + e;
+        x[e] = (s_x[0][d] + s_x[1][d]) + (s_x[2][d] + s_x[3][d]);
+      }
+      __syncthreads();
     }
-    __syncthreads();
+    if (mine == 0) {
+      const unsigned r = jn.row0 + row, t = r / unsigned(a.G);
+      const size_t oh = size_t(jn.first + t) * a.Hq + jn.g * a.G + (r - t * a.G);
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      T* out = static_cast<T*>(a.out) + oh * D + lane * CPL;
+#pragma unroll
+      for (int e = 0; e < CPL; ++e) out[e] = from_f<T>(x[e] * inv);
+      if (a.lse && lane == 0)
+        a.lse[oh] = l == 0.f ? kNegInf
+                             : ((m == kNegInf ? 0.f : m) + __builtin_amdgcn_logf(l)) * kLn2;
+    }
   }
 }
 
@@ -936,10 +988,12 @@ const void* attend_fn(int rows) {
 template <typename T, int D>
 const void* join_fn(int rows) {
   if constexpr (sizeof(T) == 4) {
-    return fn(&join_kernel<T, D, 128>);
+    return fn(&join_kernel<T, D, 128, 1>);
   } else {
-    return rows == 16 ? fn(&join_kernel<T, D, 16>) : rows == 32 ? fn(&join_kernel<T, D, 32>)
-         : rows == 128 ? fn(&join_kernel<T, D, 128>) : fn(&join_kernel<T, D, 256>);
+    return rows == 16    ? fn(&join_kernel<T, D, 16, 4>)
+           : rows == 32  ? fn(&join_kernel<T, D, 32, 4>)
+           : rows == 128 ? fn(&join_kernel<T, D, 128, 1>)
+                         : fn(&join_kernel<T, D, 256, 1>);
   }
 }
 

@@ -18,7 +18,6 @@ constexpr int kSlotTile = 64;   // cache slots of one tile; a page holds whole t
 
 C2KV_INDEX_FN int imin_(int a, int b) { return a < b ? a : b; }
 C2KV_INDEX_FN int imax_(int a, int b) { return a > b ? a : b; }
-C2KV_INDEX_FN int64_t imin64(int64_t a, int64_t b) { return a < b ? a : b; }
 
 // One request's chunk: rows [first, first + n) of the chunk tensors; its row t is cache
 // index base + t (negative where the chunk is longer than the cache's stated length).
@@ -69,31 +68,47 @@ C2KV_INDEX_FN int valid_page(int id, int n_pages) {
 // request, kv-head, row block; a unit's work is its key tiles, and the tiles of all units
 // in that order are one line that the workgroups of a launch share evenly, each a
 // contiguous stretch: whatever the lengths, all finish together.  A unit cut by a border
-// is joined afterwards.
+// is joined afterwards.  Rows (n G) and the line's tiles are below 2^31 (the host refuses
+// what could have more), so all of this is 32-bit arithmetic: a 64-bit division takes a
+// GPU about half a microsecond.
 
 // Keys that exist for row block `i` of a chunk: what its last token sees.
-C2KV_INDEX_FN int unit_keys(const Req& r, int G, int rb, int i, int limit) {
-  const int64_t last = imin64(int64_t(i + 1) * rb, int64_t(r.n) * G) - 1;
-  return int(imin64(imax_(0, r.base + int(last / G) + 1), limit));
+C2KV_INDEX_FN int unit_keys(const Req& r, unsigned G, unsigned rb, unsigned i, int limit) {
+  const unsigned rows = unsigned(r.n) * G, end = (i + 1) * rb;
+  const unsigned last = (end < rows ? end : rows) - 1;
+  return imin_(imax_(0, r.base + int(last / G) + 1), limit);
 }
 // Its tiles: at least one, so that rows that see no key are answered as well.
-C2KV_INDEX_FN int unit_tiles(const Req& r, int G, int rb, int i, int limit) {
+C2KV_INDEX_FN int unit_tiles(const Req& r, unsigned G, unsigned rb, unsigned i, int limit) {
   return imax_(1, (unit_keys(r, G, rb, i, limit) + kSlotTile - 1) / kSlotTile);
 }
-C2KV_INDEX_FN int row_blocks(const Req& r, int G, int rb) {
-  return int((int64_t(r.n) * G + rb - 1) / rb);
+C2KV_INDEX_FN int row_blocks(const Req& r, unsigned G, unsigned rb) {
+  return int((unsigned(r.n) * G + rb - 1) / rb);
 }
 // Tiles of all row blocks of one kv-head.
-C2KV_INDEX_FN int64_t head_tiles(const Req& r, int G, int rb, int limit) {
-  int64_t t = 0;
+C2KV_INDEX_FN unsigned head_tiles(const Req& r, unsigned G, unsigned rb, int limit) {
+  unsigned t = 0;
   for (int i = 0, e = row_blocks(r, G, rb); i < e; ++i) t += unit_tiles(r, G, rb, i, limit);
   return t;
 }
-// First tile of workgroup w's share of `total` tiles, and the workgroup whose share holds
-// tile x (shares of fewer tiles than workgroups are empty for some).
-C2KV_INDEX_FN int64_t share_begin(int64_t total, int W, int w) { return total * w / W; }
-C2KV_INDEX_FN int share_of(int64_t total, int W, int64_t x) {
-  return int(((x + 1) * W - 1) / total);
+// A bound on the line's tiles that the host can form: no block has more than the limit's.
+C2KV_INDEX_FN int64_t most_tiles(int64_t n_tokens, int64_t batch, int64_t G, int64_t heads,
+                                 int64_t rb, int64_t limit) {
+  return heads * (n_tokens * G / rb + batch) * imax_(1, int(limit / kSlotTile));
+}
+
+// Shares of `groups` workgroups: the first `more` have one tile more than the others.
+struct Shares {
+  unsigned total, size, more;
+  C2KV_INDEX_FN unsigned begin(unsigned w) const { return size * w + (w < more ? w : more); }
+  // workgroup whose share holds tile x
+  C2KV_INDEX_FN unsigned of(unsigned x) const {
+    const unsigned big = more * (size + 1);
+    return x < big ? x / (size + 1) : more + (x - big) / size;
+  }
+};
+C2KV_INDEX_FN Shares make_shares(unsigned total, unsigned groups) {
+  return {total, total / groups, total % groups};
 }
 
 }  // namespace c2kv

@@ -89,21 +89,21 @@ int main(int argc, char** argv) {
                             return int(ends.size()) > n ? ends[ends.size() - n - 1] : int64_t(0);
                           }()));
     }
-    if (total > 0) {
-      CHECK(share_begin(total, W, 0) == 0 && share_begin(total, W, W) == total);
+    if (good) CHECK(total <= most_tiles(n_tokens, B, G, Hkv, rb, limit));
+    if (total > 0 && total < (int64_t(1) << 31)) {
+      const Shares sh = make_shares(unsigned(total), unsigned(W));
+      CHECK(sh.begin(0) == 0 && sh.begin(W) == total);
       for (int w = 0; w < W; ++w) {
-        const int64_t p0 = share_begin(total, W, w), p1 = share_begin(total, W, w + 1);
-        CHECK(p0 <= p1);
+        const unsigned p0 = sh.begin(w), p1 = sh.begin(w + 1);
+        CHECK(p0 <= p1 && p1 - p0 <= total / W + 1);
         if (p0 == p1) continue;
-        CHECK(share_of(total, W, p0) == w && share_of(total, W, p1 - 1) == w);
+        CHECK(sh.of(p0) == unsigned(w) && sh.of(p1 - 1) == unsigned(w));
       }
       for (int64_t e : ends) {
-        const int w = share_of(total, W, e - 1);
-        CHECK(w >= 0 && w < W && share_begin(total, W, w) <= e - 1 &&
-              e - 1 < share_begin(total, W, w + 1));
+        const unsigned w = sh.of(unsigned(e - 1));
+        CHECK(w < unsigned(W) && sh.begin(w) <= e - 1 && e - 1 < sh.begin(w + 1));
       }
     }
-    if (good) CHECK(tiles <= n_tokens / kSlotTile + 2l * B);
   }
   const int it = -1;
   CHECK(valid_page(-1, 5) == -1 && valid_page(5, 5) == -1 && valid_page(4, 5) == 4);

@@ -91,11 +91,10 @@ __device__ inline Share find_share(const AttendParams& a, int w, int limit, unsi
       unsigned rest = s.p0 - seen - (of(incl) - of(cost));
       at.g = int(rest / of(head));
       rest -= at.g * of(head);
+      UnitWalk u(at.r, a.G, RB, limit);
       at.i = 0;
-      while (rest >= unsigned(at.tiles = unit_tiles(at.r, a.G, RB, at.i, limit))) {
-        rest -= at.tiles;
-        ++at.i;
-      }
+      for (; rest >= unsigned(u.tiles()); u.next(), ++at.i) rest -= u.tiles();
+      at.tiles = u.tiles();
       at.tile = int(rest);
       return s;
     }
@@ -150,27 +149,30 @@ struct Piece {
 // rows
 // ----------------------------------------------------------------------------
 
-// 8 consecutive elements d0 .. d0 + 7 of a query row, turned to pos and scaled
-template <typename T, int D>
-__device__ inline void query8(const AttendParams& a, const T* row, int d0, int pos,
-                              float (&out)[8]) {
-  const int lo = d0 % (D / 2);
-  if (!a.rope.pos) {
-    load8(row + d0, out);
-  } else {
-    float x[8], y[8];
-    load8(row + lo, x);
-    load8(row + lo + D / 2, y);
+// Turns per position of the pairs, from the kernel's arguments into LDS.
+template <int D>
+__device__ inline void stage_turns(const AttendParams& a, double* turns) {
+  if (threadIdx.x < D / 2) turns[threadIdx.x] = a.rope.turns[threadIdx.x];
+}
+
+// Two chunks of N elements of a query row that RoPE pairs, D / 2 apart, turned to pos and
+// scaled in fp32.
+template <int N>
+__device__ inline void turn_chunks(const double* turns, bool on, int pos, float scale,
+                                   float (&x)[N], float (&y)[N]) {
+  if (on) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < N; ++e) {
       float c, s;
-      turn_cs(pos, a.rope.turns[lo + e], c, s);
+      turn_cs(pos, turns[e], c, s);
       rotate_pair(x[e], y[e], c, s);
-      out[e] = d0 < D / 2 ? x[e] : y[e];
     }
   }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) out[e] *= a.qscale;
+  for (int e = 0; e < N; ++e) {
+    x[e] *= scale;
+    y[e] *= scale;
+  }
 }
 
 __device__ inline bf16x8 bf16_of(const float (&x)[8]) {
@@ -227,10 +229,12 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
 
   __shared__ __attribute__((aligned(16))) float s_o[NW * RB * LDO];
   __shared__ float s_m[NW * RB], s_l[NW * RB];
+  __shared__ double s_turns[D / 2];
 
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
   const int col = lane & 15, j = lane >> 4;
   const int PS = a.pg.PS, limit = a.ch.max_pages * PS;
+  stage_turns<D>(a, s_turns);
   // (fewer tiles a workgroup would leave wavefronts without a step)
   Place at;
   const Share share = find_share<RB>(a, blockIdx.x, limit, I8 ? 4 : 2, at);
@@ -292,16 +296,38 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
       x.vs = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(vsr, 4 * lane, 0, 0));
     }
   };
-  // a piece's first steps
+  // query chunk c of a lane: elements qd(c) .. + 7, following the keys' 16-byte pieces; its
+  // partner is chunk c + NQP of the lane, or, where two lanes hold the pair, only loaded
+  constexpr int NQP = I8 && D == 64 ? NQC : NQC / 2;
+  auto qd = [&](int c) __attribute__((always_inline)) {
+    return I8 ? 64 * (c / 2) + 16 * j + 8 * (c % 2) : 32 * c + 8 * j;
+  };
+  uint32_t qx[NB][NQP][4], qy[NB][NQP][4];
+  int qpos[NB], qt[NB];                      // position, and token of the chunk
+  // a piece's queries and first steps
   auto enter = [&]() __attribute__((always_inline)) {
     const int n = (cur.t1 - cur.t0) * SPT;
     s0 = cur.t0 * SPT + n * wave / NW;
     s1 = cur.t0 * SPT + n * (wave + 1) / NW;
     fetch_ids(s0 / SPT);
 #pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const unsigned row = cur.row0 + min(16 * nb + col, cur.nrows - 1);
+      qt[nb] = row / unsigned(a.G);
+      const T* qrow = static_cast<const T*>(a.q) + (cur.r.first + qt[nb]) * a.q_stride +
+                      size_t(cur.g * a.G + row - qt[nb] * a.G) * D;
+      qpos[nb] = a.rope.pos ? a.rope.pos[cur.r.first + qt[nb]] : 0;
+#pragma unroll
+      for (int c = 0; c < NQP; ++c) {
+        raw_load8<T>(qx[nb][c], qrow + qd(c) % (D / 2));
+        raw_load8<T>(qy[nb][c], qrow + qd(c) % (D / 2) + D / 2);
+      }
+    }
+#pragma unroll
     for (int k = 0; k < SETS; ++k) fetch(s0 + k, set[k]);
   };
   enter();
+  lds_barrier();                             // the turns are there
 
   while (true) {
     // ---- queries: turned by their tokens' positions, the softmax scale folded in
@@ -309,18 +335,20 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
     int sees[NB];                            // keys that this lane's rows see
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      const unsigned row = cur.row0 + min(16 * nb + col, cur.nrows - 1);
-      const int t = row / unsigned(a.G);
-      sees[nb] = min(max(cur.r.base + t + 1, 0), limit);
-      const T* qrow = static_cast<const T*>(a.q) + (cur.r.first + t) * a.q_stride +
-                      size_t(cur.g * a.G + row - t * a.G) * D;
-      const int pos = a.rope.pos ? a.rope.pos[cur.r.first + t] : 0;
+      sees[nb] = min(max(cur.r.base + qt[nb] + 1, 0), limit);
 #pragma unroll
-      for (int c = 0; c < NQC; ++c) {
-        float x[8];
-        // the contraction index follows the keys' 16-byte pieces
-        query8<T, D>(a, qrow, I8 ? 64 * (c / 2) + 16 * j + 8 * (c % 2) : 32 * c + 8 * j, pos, x);
-        q[nb][c] = bf16_of(x);
+      for (int c = 0; c < NQP; ++c) {
+        float x[8], y[8];
+        raw_to_f8<T>(qx[nb][c], x);
+        raw_to_f8<T>(qy[nb][c], y);
+        turn_chunks<8>(s_turns + qd(c) % (D / 2), a.rope.pos, qpos[nb], a.qscale, x, y);
+        if constexpr (NQP < NQC) {
+          q[nb][c] = bf16_of(x);
+          q[nb][c + NQP] = bf16_of(y);
+        } else {
+          const bf16x8 lo = bf16_of(x), hi = bf16_of(y);
+          q[nb][c] = qd(c) < D / 2 ? lo : hi;
+        }
       }
     }
     const int sees_all = min(max(cur.r.base + int(unsigned(cur.row0) / unsigned(a.G)) + 1, 0),
@@ -583,6 +611,7 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
                 "a thread's chunks of one tile lie in rows of one permutation");
 
   __shared__ __attribute__((aligned(1024))) uint8_t lds[NST * W::BYTES];
+  __shared__ double s_turns[D / 2];
   const uint32_t lds0 = uint32_t(uintptr_t((__attribute__((address_space(3))) uint8_t*)lds));
 
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
@@ -593,10 +622,12 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
   const int nx = gridDim.x / 8;
   const int w = gridDim.x % 8 == 0 ? int(blockIdx.x % 8) * nx + int(blockIdx.x / 8)
                                    : int(blockIdx.x);
+  stage_turns<D>(a, s_turns);
   Place at;
   const Share share = find_share<RB>(a, w, limit, 2, at);
   Join join{};
   unsigned p = share.p0;
+  lds_barrier();                                 // the turns are there
 
   // this thread's chunks of a tile: chunk tid + i * 512 of the keys, and of the values
   const int kkey = tid / W::CK, kch = (tid % W::CK) ^ (kkey & W::MK);
@@ -639,35 +670,42 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
 
     // ---- this wavefront's rows
     const bool rows_here = 32 * rg < nrows;
-    const int row = row0 + min(32 * rg + col, nrows - 1), t = row / a.G;
-    const int sees = min(max(at.r.base + t + 1, 0), limit);
+    const unsigned row = row0 + min(32 * rg + col, nrows - 1), t = row / unsigned(a.G);
+    const int sees = min(max(at.r.base + int(t) + 1, 0), limit);
     // every row's keys, and any row's
-    const int wrow0 = row0 + min(32 * rg, nrows - 1);
-    const int sees_all = min(max(at.r.base + wrow0 / a.G + 1, 0), limit);
-    const int wrow1 = row0 + min(32 * rg + 31, nrows - 1);
-    const int sees_any = min(max(at.r.base + wrow1 / a.G + 1, 0), limit);
+    auto token_of = [&](int r) { return int(unsigned(row0 + min(r, nrows - 1)) / unsigned(a.G)); };
+    const int sees_all = min(max(at.r.base + token_of(32 * rg) + 1, 0), limit);
+    const int sees_any = min(max(at.r.base + token_of(32 * rg + 31) + 1, 0), limit);
     typename M::Op q[NQC * (F32 ? 4 : 1)];
     {
       const T* qrow = static_cast<const T*>(a.q) + (at.r.first + t) * a.q_stride +
                       size_t(at.g * a.G + row % a.G) * D;
       const int pos = a.rope.pos ? a.rope.pos[at.r.first + t] : 0;
       // chunk 2 c + half of the row; its partner D / 2 away is chunk c + NQC / 2's
+      uint4 qx[NQC / 2], qy[NQC / 2];
 #pragma unroll
       for (int c = 0; c < NQC / 2; ++c) {
-        const int d0 = (2 * c + half) * W::EPC;
-        float x[W::EPC], y[W::EPC];
+        const T* from = qrow + (2 * c + half) * W::EPC;
+        qx[c] = *reinterpret_cast<const uint4*>(from);
+        qy[c] = *reinterpret_cast<const uint4*>(from + D / 2);
+      }
 #pragma unroll
-        for (int e = 0; e < W::EPC; ++e) {
-          x[e] = to_f(qrow[d0 + e]);
-          y[e] = to_f(qrow[d0 + D / 2 + e]);
-          if (a.rope.pos) {
-            float cc, ss;
-            turn_cs(pos, a.rope.turns[d0 + e], cc, ss);
-            rotate_pair(x[e], y[e], cc, ss);
-          }
-          x[e] *= a.qscale;
-          y[e] *= a.qscale;
+      for (int c = 0; c < NQC / 2; ++c) {
+        float x[W::EPC], y[W::EPC];
+        if constexpr (F32) {
+          const float xs[4] = {__uint_as_float(qx[c].x), __uint_as_float(qx[c].y),
+                               __uint_as_float(qx[c].z), __uint_as_float(qx[c].w)};
+          const float ys[4] = {__uint_as_float(qy[c].x), __uint_as_float(qy[c].y),
+                               __uint_as_float(qy[c].z), __uint_as_float(qy[c].w)};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) { x[e] = xs[e]; y[e] = ys[e]; }
+        } else {
+          const uint32_t xs[4] = {qx[c].x, qx[c].y, qx[c].z, qx[c].w};
+          const uint32_t ys[4] = {qy[c].x, qy[c].y, qy[c].z, qy[c].w};
+          raw_to_f8<T>(xs, x);
+          raw_to_f8<T>(ys, y);
         }
+        turn_chunks<W::EPC>(s_turns + (2 * c + half) * W::EPC, a.rope.pos, pos, a.qscale, x, y);
         if constexpr (F32) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
@@ -899,7 +937,7 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
 // few (PW = 1).
 template <typename T, int D, int RB, int PW>
 __global__ __launch_bounds__(256) void join_kernel(AttendParams a) {
-  constexpr int CPL = D / 64, NW = 4, N = 8; // columns of a lane; pieces in flight
+  constexpr int CPL = D / 64, NW = 4, N = PW > 1 ? 16 : 8;   // columns of a lane; pieces in flight
   __shared__ float s_x[NW][D];
   const int w0 = blockIdx.x, wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const Join jn = a.joins[w0];

@@ -72,23 +72,48 @@ C2KV_INDEX_FN int valid_page(int id, int n_pages) {
 // what could have more), so all of this is 32-bit arithmetic: a 64-bit division takes a
 // GPU about half a microsecond.
 
-// Keys that exist for row block `i` of a chunk: what its last token sees.
-C2KV_INDEX_FN int unit_keys(const Req& r, unsigned G, unsigned rb, unsigned i, int limit) {
-  const unsigned rows = unsigned(r.n) * G, end = (i + 1) * rb;
-  const unsigned last = (end < rows ? end : rows) - 1;
-  return imin_(imax_(0, r.base + int(last / G) + 1), limit);
-}
-// Its tiles: at least one, so that rows that see no key are answered as well.
-C2KV_INDEX_FN int unit_tiles(const Req& r, unsigned G, unsigned rb, unsigned i, int limit) {
-  return imax_(1, (unit_keys(r, G, rb, i, limit) + kSlotTile - 1) / kSlotTile);
-}
 C2KV_INDEX_FN int row_blocks(const Req& r, unsigned G, unsigned rb) {
   return int((unsigned(r.n) * G + rb - 1) / rb);
+}
+// The row blocks of a chunk in turn; divides once, not per block.
+struct UnitWalk {
+  unsigned G, step, step_rest;       // tokens from one block's last row to the next's
+  unsigned token, rest;              // of the block's last row, as if all blocks were full
+  int base, last, limit;
+
+  C2KV_INDEX_FN UnitWalk(const Req& r, unsigned G_, unsigned rb, int limit_, unsigned i = 0)
+      : G(G_), step(rb / G_), step_rest(rb % G_), base(r.base), last(r.n - 1), limit(limit_) {
+    const unsigned row = (i + 1) * rb - 1;
+    token = row / G;
+    rest = row % G;
+  }
+  C2KV_INDEX_FN void next() {
+    token += step;
+    rest += step_rest;
+    if (rest >= G) {
+      rest -= G;
+      ++token;
+    }
+  }
+  // keys that exist for the block: what its last token sees
+  C2KV_INDEX_FN int keys() const {
+    const int t = token < unsigned(last) ? int(token) : last;
+    return imin_(imax_(0, base + t + 1), limit);
+  }
+  // its tiles: at least one, so that rows that see no key are answered as well
+  C2KV_INDEX_FN int tiles() const { return imax_(1, (keys() + kSlotTile - 1) / kSlotTile); }
+};
+C2KV_INDEX_FN int unit_keys(const Req& r, unsigned G, unsigned rb, unsigned i, int limit) {
+  return UnitWalk(r, G, rb, limit, i).keys();
+}
+C2KV_INDEX_FN int unit_tiles(const Req& r, unsigned G, unsigned rb, unsigned i, int limit) {
+  return UnitWalk(r, G, rb, limit, i).tiles();
 }
 // Tiles of all row blocks of one kv-head.
 C2KV_INDEX_FN unsigned head_tiles(const Req& r, unsigned G, unsigned rb, int limit) {
   unsigned t = 0;
-  for (int i = 0, e = row_blocks(r, G, rb); i < e; ++i) t += unit_tiles(r, G, rb, i, limit);
+  UnitWalk u(r, G, rb, limit);
+  for (int i = row_blocks(r, G, rb); i > 0; --i, u.next()) t += unsigned(u.tiles());
   return t;
 }
 // A bound on the line's tiles that the host can form: no block has more than the limit's.

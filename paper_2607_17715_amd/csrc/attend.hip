@@ -726,46 +726,23 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
 #pragma unroll
     for (int db = 0; db < NDB; ++db) o[db] = bias;
 
-    auto compute = [&](int tile, int page, const uint8_t* st) __attribute__((always_inline)) {
-      f32x16 s[NKB];
-      // ---- scores (relative to the reference: the chains begin with minus it)
+    // value v of a 32-key block is its key 16 (v / 8) + 8 half + v % 8 (fp32: 8 (v / 4) +
+    // 4 half + v % 4); block b of this wavefront's part of the tile
+    auto mask = [&](int tile, int b, int page, f32x16& s) __attribute__((always_inline)) {
+      const int k0 = tile * ST + 32 * (kg * NKB + b);
+      if (k0 + 32 <= sees_all && page >= 0) return;
+      const int lim = page < 0 ? -64 : sees - k0 - (F32 ? 4 : 8) * half - 1;
 #pragma unroll
-      for (int b = 0; b < NKB; ++b) {
-        const int kr = 32 * (kg * NKB + b) +
-                       (F32 ? col : (col & ~12) | (col & 4) << 1 | (col & 8) >> 1);
-        s[b] = bias;
-#pragma unroll
-        for (int c = 0; c < NQC; ++c) {
-          const uint8_t* from = st + W::k_at(kr, 2 * c + half);
-          if constexpr (F32) {
-            const float4 f = *reinterpret_cast<const float4*>(from);
-            s[b] = M::run(f.x, q[4 * c], s[b]);
-            s[b] = M::run(f.y, q[4 * c + 1], s[b]);
-            s[b] = M::run(f.z, q[4 * c + 2], s[b]);
-            s[b] = M::run(f.w, q[4 * c + 3], s[b]);
-          } else {
-            s[b] = M::run(*reinterpret_cast<const bf16x8*>(from), q[c], s[b]);
-          }
-        }
+      for (int v = 0; v < 16; ++v) {
+        const int key = F32 ? 8 * (v >> 2) + (v & 3) : 16 * (v >> 3) + (v & 7);
+        const uint32_t hide = uint32_t((lim - key) >> 31);
+        const uint32_t x = __float_as_uint(s[v]);
+        s[v] = __uint_as_float((x & ~hide) | (0xff800000u & hide));
       }
-      // value v of block b is key 32 b + 16 (v / 8) + 8 half + v % 8 (fp32: 8 (v / 4) +
-      // 4 half + v % 4) of the wavefront's part
-      const int k0 = tile * ST + 32 * kg * NKB;
-      if (k0 + 32 * NKB > sees_all || page < 0) {
-        const int lim = page < 0 ? -64 : sees - k0 - (F32 ? 4 : 8) * half - 1;
-#pragma unroll
-        for (int b = 0; b < NKB; ++b)
-#pragma unroll
-          for (int v = 0; v < 16; ++v) {
-            const int key = 32 * b + (F32 ? 8 * (v >> 2) + (v & 3) : 16 * (v >> 3) + (v & 7));
-            const uint32_t hide = uint32_t((lim - key) >> 31);
-            const uint32_t x = __float_as_uint(s[b][v]);
-            s[b][v] = __uint_as_float((x & ~hide) | (0xff800000u & hide));
-          }
-      }
-      float mx = s[0][0];
-#pragma unroll
-      for (int i = 1; i < 16 * NKB; ++i) mx = fmaxf(mx, s[i / 16][i % 16]);
+    };
+    // the reference moves where a score outgrows it (by mx) by over kLazyLog2; scores are
+    // relative to it: the MFMA chains begin with `bias`, minus it
+    auto rebase = [&](float mx, f32x16 (&s)[NKB]) __attribute__((always_inline)) {
       if (__any(mx + m_ref > m_run + kLazyLog2)) {
         const float m_new = fmaxf(m_run, half_pair_max(mx) + m_ref);
         const float ref = m_new == kNegInf ? 0.f : m_new;
@@ -784,14 +761,68 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
         m_run = m_new;
         m_ref = ref;
       }
-      // ---- probabilities and P*V
+    };
+    auto stage = [&](int tile) { return lds + (tile - t0) % NST * W::BYTES; };
+    // what lies behind the last key may be anything: zero values there
+    auto clean = [&](int tile, int page) __attribute__((always_inline)) {
+      if ((tile + 1) * ST <= keys && page >= 0) return;
+      const int n = page < 0 ? 0 : max(keys - tile * ST, 0);
+#pragma unroll
+      for (int i = 0; i < LV; ++i) {
+        uint4* v = reinterpret_cast<uint4*>(stage(tile) + W::KBYTES + (tid + i * NTH) * 16);
+        if (vch * W::EPC + W::EPC > n) *v = keep_first<T>(*v, max(n - vch * W::EPC, 0));
+      }
+      lds_barrier();
+    };
+    // ---- one tile: scores, probabilities, P*V
+    auto compute = [&](int tile, int page, const uint8_t* st) __attribute__((always_inline)) {
+      f32x16 s[NKB];
+      if constexpr (F32) {
+        static_assert(!F32 || NKB == 1, "an fp32 wavefront has one block of a tile");
+        s[0] = bias;
+#pragma unroll
+        for (int c = 0; c < NQC; ++c) {
+          const float4 f =
+              *reinterpret_cast<const float4*>(st + W::k_at(32 * kg + col, 2 * c + half));
+          s[0] = M::run(f.x, q[4 * c], s[0]);
+          s[0] = M::run(f.y, q[4 * c + 1], s[0]);
+          s[0] = M::run(f.z, q[4 * c + 2], s[0]);
+          s[0] = M::run(f.w, q[4 * c + 3], s[0]);
+        }
+      } else {
+        // operands in a ring AH ahead of their MFMAs; the scheduling fences hold the order
+        constexpr int NF = NKB * NQC, AH = 4;
+        const int kr = 32 * kg * NKB + ((col & ~12) | (col & 4) << 1 | (col & 8) >> 1);
+        auto frag = [&](int f) __attribute__((always_inline)) {
+          return *reinterpret_cast<const bf16x8*>(
+              st + W::k_at(kr + 32 * (f / NQC), 2 * (f % NQC) + half));
+        };
+        bf16x8 kf[AH];
+#pragma unroll
+        for (int f = 0; f < AH; ++f) kf[f] = frag(f);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);           // matrix work before the other's softmax
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+          const int b = f / NQC, c = f % NQC;
+          s[b] = M::run(kf[f % AH], q[c], c == 0 ? bias : s[b]);
+          if (f + AH < NF) kf[f % AH] = frag(f + AH);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_s_setprio(0);
+      }
+#pragma unroll
+      for (int b = 0; b < NKB; ++b) mask(tile, b, page, s[b]);
+      float mx = s[0][0];
+#pragma unroll
+      for (int i = 1; i < 16 * NKB; ++i) mx = fmaxf(mx, s[i / 16][i % 16]);
+      rebase(mx, s);
       float sum[4] = {0.f, 0.f, 0.f, 0.f};
       if constexpr (F32) {
 #pragma unroll
-        for (int i = 0; i < 16 * NKB; ++i) {
-          const float x = __builtin_amdgcn_exp2f(s[i / 16][i % 16]);
-          s[i / 16][i % 16] = x;
-          sum[i % 4] += x;
+        for (int i = 0; i < 16; ++i) {
+          s[0][i] = __builtin_amdgcn_exp2f(s[0][i]);
+          sum[i % 4] += s[0][i];
         }
         // a tile's sum apart, then added: the rounding of a long sum grows with the tiles
 #pragma unroll
@@ -803,10 +834,10 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
           for (int c = 0; c < NPC; ++c) {
             const float4 f = *reinterpret_cast<const float4*>(
                 st + W::v_at(32 * db + col, 2 * (kg * NPC + c) + half));
-            part = M::run(f.x, s[c / 4][4 * (c % 4)], part);
-            part = M::run(f.y, s[c / 4][4 * (c % 4) + 1], part);
-            part = M::run(f.z, s[c / 4][4 * (c % 4) + 2], part);
-            part = M::run(f.w, s[c / 4][4 * (c % 4) + 3], part);
+            part = M::run(f.x, s[0][4 * c], part);
+            part = M::run(f.y, s[0][4 * c + 1], part);
+            part = M::run(f.z, s[0][4 * c + 2], part);
+            part = M::run(f.w, s[0][4 * c + 3], part);
           }
           o[db] += part;
         }
@@ -825,17 +856,29 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
             // the sum of the rounded values that the product uses
             sum[e / 2] = __builtin_amdgcn_fdot2_f32_bf16(b, ones, sum[e / 2], false);
           }
+        constexpr int NF = NPC * NDB, AH = 4;
+        auto frag = [&](int f) __attribute__((always_inline)) {
+          return *reinterpret_cast<const bf16x8*>(
+              st + W::v_at(32 * (f % NDB) + col, 2 * (kg * NPC + f / NDB) + half));
+        };
+        bf16x8 vf[AH];
 #pragma unroll
-        for (int c = 0; c < NPC; ++c)
+        for (int f = 0; f < AH; ++f) vf[f] = frag(f);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-          for (int db = 0; db < NDB; ++db)
-            o[db] = M::run(*reinterpret_cast<const bf16x8*>(
-                               st + W::v_at(32 * db + col, 2 * (kg * NPC + c) + half)),
-                           pb[c], o[db]);
+        for (int f = 0; f < NF; ++f) {
+          o[f % NDB] = M::run(vf[f % AH], pb[f / NDB], o[f % NDB]);
+          if (f + AH < NF) vf[f % AH] = frag(f + AH);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_s_setprio(0);
       }
       l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     };
 
+    // tiles [t0, end) have keys that rows of this wavefront see
+    const int end = rows_here ? (sees_any + ST - 1) / ST : t0;
     for (int tile = t0; tile < t1; ++tile) {
       // this tile's loads are done where only those of the tiles after it are in flight
       const int after = min(t1 - 1 - tile, NST - 2);
@@ -844,19 +887,9 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
       else wait_loads_barrier<0>();
       // (every wavefront is past the tile before, whose place the next load takes)
       if (tile + NST - 1 < t1) load(tile + NST - 1);
-      uint8_t* st = lds + (tile - t0) % NST * W::BYTES;
       const int page = page_id(tile);
-      if ((tile + 1) * ST > keys || page < 0) {
-        // what lies behind the last key may be anything: zero values there
-        const int n = page < 0 ? 0 : max(keys - tile * ST, 0);
-#pragma unroll
-        for (int i = 0; i < LV; ++i) {
-          uint4* v = reinterpret_cast<uint4*>(st + W::KBYTES + (tid + i * NTH) * 16);
-          if (vch * W::EPC + W::EPC > n) *v = keep_first<T>(*v, max(n - vch * W::EPC, 0));
-        }
-        lds_barrier();
-      }
-      if (rows_here && tile * ST < sees_any) compute(tile, page, st);
+      clean(tile, page);
+      if (tile < end) compute(tile, page, stage(tile));
     }
 
     // ---- the key parts of a row group meet

@@ -9,6 +9,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <utility>
 
 #include "cache.hpp"
 #include "cache_device.hpp"
@@ -192,11 +193,11 @@ __device__ inline void lds_barrier() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
-// value of lane k of this lane's group of 16 (a DPP operand of what uses it)
-template <int K>
-__device__ inline float lane16(float x) {
-  return __uint_as_float(__builtin_amdgcn_update_dpp(0, int(__float_as_uint(x)), 0x150 + K, 0xf,
-                                                     0xf, true));
+// values of the 16 lanes of this lane's group (DPP operands of what uses them)
+template <int... K>
+__device__ inline void lanes16(float x, float (&v)[16], std::integer_sequence<int, K...>) {
+  ((v[K] = __uint_as_float(__builtin_amdgcn_update_dpp(0, int(__float_as_uint(x)), 0x150 + K,
+                                                       0xf, 0xf, true))), ...);
 }
 
 // ----------------------------------------------------------------------------
@@ -400,16 +401,13 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
       }
       if constexpr (I8) {
         // lane l has the scale of key key0 + l, and scores of its group's 16 keys
-        auto scaled = [&](auto k_c) __attribute__((always_inline)) {
-          constexpr int k = decltype(k_c)::value;
+        float ks[16];
+        lanes16(x.ks, ks, std::make_integer_sequence<int, 16>{});
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
-            s[nb][k / 4][k % 4] =
-                __builtin_fmaf(s[nb][k / 4][k % 4], lane16<k>(x.ks), -m_ref[nb]);
-        };
-        [&]<int... k>(std::integer_sequence<int, k...>) __attribute__((always_inline)) {
-          (scaled(std::integral_constant<int, k>{}), ...);
-        }(std::make_integer_sequence<int, 16>{});
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int k = 0; k < 16; ++k)
+            s[nb][k / 4][k % 4] = __builtin_fmaf(s[nb][k / 4][k % 4], ks[k], -m_ref[nb]);
       }
       if (partial) {
 #pragma unroll
@@ -460,9 +458,10 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
         }
         l_run[nb] += sum;
         if constexpr (I8) {
-          [&]<int... k>(std::integer_sequence<int, k...>) __attribute__((always_inline)) {
-            ((pr[k] *= lane16<k>(x.vs)), ...);
-          }(std::make_integer_sequence<int, 16>{});
+          float vs[16];
+          lanes16(x.vs, vs, std::make_integer_sequence<int, 16>{});
+#pragma unroll
+          for (int k = 0; k < 16; ++k) pr[k] *= vs[k];
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -592,16 +591,20 @@ __device__ inline void wait_loads_barrier() {
 // Scores transposed (keys x rows) in 32x32 MFMAs: a lane has one row's scores, for bf16 of
 // 8 consecutive keys at a time (keys are dealt to the MFMA's rows with bits 2 and 3 of
 // their index exchanged), the operand of the P*V product.
-template <typename T, int D, int RG>
+//
+// int8 tiles go through registers, decoded (code * scale in fp32) and rounded to bf16 once,
+// as c2kv_compose decodes them: applied to scores and probabilities instead, the scales
+// would cost every wavefront what here costs the workgroup once.
+template <typename T, typename S, int D, int RG>
 __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
   using M = Mma<T>;
   using W = WideTile<T, D>;
-  constexpr bool F32 = sizeof(T) == 4;
+  constexpr bool F32 = sizeof(T) == 4, I8 = sizeof(S) == 1;
   constexpr int SZ = sizeof(T), NTH = 512;
   constexpr int KG = 8 / RG, NKB = 2 / KG;       // key parts, 32-key blocks of a wavefront
   static_assert(KG <= 2, "a wavefront has a 32-key block at least");
   constexpr int RB = 32 * RG;
-  constexpr int NST = F32 ? 2 : 4;               // tiles in LDS
+  constexpr int NST = F32 || I8 ? 2 : 4;         // tiles in LDS
   constexpr int LK = ST * W::CK / NTH, LV = D * W::CV / NTH, LPT = LK + LV;
   constexpr int NQC = W::CK / 2;                 // query chunks of a lane (its half's)
   constexpr int NPC = 16 * NKB / W::EPC;         // probability chunks of a lane
@@ -610,7 +613,10 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
                     (NTH / W::CV) % (W::MV + 1) == 0,
                 "a thread's chunks of one tile lie in rows of one permutation");
 
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[NST * W::BYTES];
+  constexpr int XW = 2 + 16 * NDB;               // what key parts exchange: floats a lane
+  constexpr int XBYTES = KG == 2 ? RG * 64 * XW * 4 : 0;
+  __shared__ __attribute__((aligned(1024)))
+  uint8_t lds[NST * W::BYTES > XBYTES ? NST * W::BYTES : XBYTES];
   __shared__ double s_turns[D / 2];
   const uint32_t lds0 = uint32_t(uintptr_t((__attribute__((address_space(3))) uint8_t*)lds));
 
@@ -663,10 +669,63 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
         load_to_lds(vp + size_t(i) * (NTH / W::CV) * PS, vofs, to + W::KBYTES + i * NTH * 16);
     };
 
-    // ---- the first tiles
+    auto stage = [&](int tile) { return lds + (tile - t0) % NST * W::BYTES; };
+    // keys of a tile that exist
+    auto there = [&](int tile, int page) { return page < 0 ? 0 : min(max(keys - tile * ST, 0), ST); };
+
+    // int8: BPT codes of a key (elements kd ..) and of a value row (keys vk ..) a thread
+    constexpr int BPT = ST * D / NTH;
+    const int ikey = tid / (D / BPT), ikd = tid % (D / BPT) * BPT;
+    const int ivd = tid / (ST / BPT), ivk = tid % (ST / BPT) * BPT;
+    uint32_t kraw[BPT / 4], vraw[BPT / 4];
+    float kscale = 0.f, vscale[BPT];
+    auto load_i8 = [&](int tile) __attribute__((always_inline)) {
+      const int page = max(page_id(tile), 0), off = tile * ST % PS;
+      const size_t ph = size_t(page) * a.pg.Hkv + at.g;
+      const int8_t* kp = static_cast<const int8_t*>(a.pg.k) + (ph * PS + off + ikey) * D + ikd;
+      const int8_t* vp = static_cast<const int8_t*>(a.pg.v) + (ph * D + ivd) * PS + off + ivk;
+      const float* sp = a.pg.v_scale + ph * PS + off + ivk;
 #pragma unroll
-    for (int k = 0; k < NST - 1; ++k)
-      if (t0 + k < t1) load(t0 + k);
+      for (int i = 0; i < BPT / 8; ++i) {
+        raw_load8<int8_t>(kraw + 2 * i, kp + 8 * i);
+        raw_load8<int8_t>(vraw + 2 * i, vp + 8 * i);
+        float x[8];
+        load8(sp + 8 * i, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vscale[8 * i + e] = x[e];
+      }
+      kscale = a.pg.k_scale[ph * PS + off + ikey];
+    };
+    auto commit_i8 = [&](int tile) __attribute__((always_inline)) {
+      const int n = there(tile, page_id(tile));
+      if (n < ST) {                              // (a scale behind the last key may be anything)
+#pragma unroll
+        for (int e = 0; e < BPT; ++e) vscale[e] = ivk + e < n ? vscale[e] : 0.f;
+      }
+      uint8_t* st = stage(tile);
+#pragma unroll
+      for (int i = 0; i < BPT / 8; ++i) {
+        float x[8], y[8];
+        raw_to_f8<int8_t>(kraw + 2 * i, x);
+        raw_to_f8<int8_t>(vraw + 2 * i, y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          x[e] *= kscale;
+          y[e] *= vscale[8 * i + e];
+        }
+        *reinterpret_cast<bf16x8*>(st + W::k_at(ikey, ikd / 8 + i)) = bf16_of(x);
+        *reinterpret_cast<bf16x8*>(st + W::v_at(ivd, ivk / 8 + i)) = bf16_of(y);
+      }
+    };
+
+    // ---- the first tiles
+    if constexpr (I8) {
+      load_i8(t0);
+    } else {
+#pragma unroll
+      for (int k = 0; k < NST - 1; ++k)
+        if (t0 + k < t1) load(t0 + k);
+    }
 
     // ---- this wavefront's rows
     const bool rows_here = 32 * rg < nrows;
@@ -762,11 +821,10 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
         m_ref = ref;
       }
     };
-    auto stage = [&](int tile) { return lds + (tile - t0) % NST * W::BYTES; };
     // what lies behind the last key may be anything: zero values there
     auto clean = [&](int tile, int page) __attribute__((always_inline)) {
-      if ((tile + 1) * ST <= keys && page >= 0) return;
-      const int n = page < 0 ? 0 : max(keys - tile * ST, 0);
+      const int n = there(tile, page);
+      if (n == ST) return;
 #pragma unroll
       for (int i = 0; i < LV; ++i) {
         uint4* v = reinterpret_cast<uint4*>(stage(tile) + W::KBYTES + (tid + i * NTH) * 16);
@@ -879,7 +937,16 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
 
     // tiles [t0, end) have keys that rows of this wavefront see
     const int end = rows_here ? (sees_any + ST - 1) / ST : t0;
-    for (int tile = t0; tile < t1; ++tile) {
+    if constexpr (I8) {
+      commit_i8(t0);
+      if (t0 + 1 < t1) load_i8(t0 + 1);
+      for (int tile = t0; tile < t1; ++tile) {
+        lds_barrier();                           // this tile is there, the one before is read
+        if (tile + 1 < t1) commit_i8(tile + 1);
+        if (tile + 2 < t1) load_i8(tile + 2);
+        if (tile < end) compute(tile, page_id(tile), stage(tile));
+      }
+    } else for (int tile = t0; tile < t1; ++tile) {
       // this tile's loads are done where only those of the tiles after it are in flight
       const int after = min(t1 - 1 - tile, NST - 2);
       if (after >= 2) wait_loads_barrier<2 * LPT>();
@@ -895,8 +962,6 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
     // ---- the key parts of a row group meet
     float l_tot = half_pair_sum(l_run);
     if constexpr (KG == 2) {
-      constexpr int XW = 2 + 16 * NDB;
-      static_assert(RG * 64 * XW * 4 <= NST * W::BYTES, "the exchange fits in the stages");
       lds_barrier();
       float* mine = reinterpret_cast<float*>(lds) + (rg * 64 + lane) * XW;
       if (kg == 1) {
@@ -1046,13 +1111,11 @@ const void* fn(K* k) { return reinterpret_cast<const void*>(k); }
 template <typename T, typename S, int D>
 const void* attend_fn(int rows) {
   if constexpr (sizeof(S) == 4) {
-    return fn(&attend_wide_kernel<T, D, 4>);
+    return fn(&attend_wide_kernel<T, S, D, 4>);
   } else {
     if (rows == 16) return fn(&attend_narrow_kernel<S, D, 1>);
     if (rows == 32) return fn(&attend_narrow_kernel<S, D, 2>);
-    if constexpr (sizeof(S) == 2)
-      return rows == 128 ? fn(&attend_wide_kernel<T, D, 4>) : fn(&attend_wide_kernel<T, D, 8>);
-    return nullptr;
+    return rows == 128 ? fn(&attend_wide_kernel<T, S, D, 4>) : fn(&attend_wide_kernel<T, S, D, 8>);
   }
 }
 
@@ -1075,7 +1138,7 @@ AttendShape attend_shape(int store, int D, int64_t rows_max, int64_t batch, int6
   AttendShape s{};
   auto up = [](size_t x) { return (x + 255) & ~size_t(255); };
   if (store == C2KV_F32) s.rows = 128;
-  else s.rows = rows_max <= 16 ? 16 : rows_max <= 32 || store == C2KV_I8 ? 32 : rows_max <= 128 ? 128 : 256;
+  else s.rows = rows_max <= 16 ? 16 : rows_max <= 32 ? 32 : rows_max <= 128 ? 128 : 256;
   const int64_t tiles =
       batch * heads * ((rows_max + s.rows - 1) / s.rows) * ((kv_max + ST - 1) / ST);
   const int64_t most = s.rows <= 32 ? 512 : 256;   // two workgroups a CU, or one

@@ -306,7 +306,7 @@ def pool_desc(k, v, k_scale=None, v_scale=None) -> PoolDesc:
         raise ValueError("pool K and V must have the same dtype and shape")
     desc = PoolDesc(code, _dev_ptr(k), _dev_ptr(v), _dev_ptr(k_scale), _dev_ptr(v_scale),
                     int(k.shape[0]))
-    desc.row_shape, desc.device = tuple(k.shape[1:]), k.device
+    desc.row_shape, desc.dev = tuple(k.shape[1:]), k.get_device()
     return desc
 
 
@@ -375,7 +375,7 @@ class Cache:
                 raise ValueError("scales must be float32 [n_pages][H_kv][page_size]")
         self.tensors = (k, v, k_scale, v_scale)
         self.device = _one_device(*self.tensors)
-        self.heads, self.head_dim = heads, d
+        self.dev, self.heads, self.head_dim = self.device.index, heads, d
         self.desc = CacheDesc(code, *(_dev_ptr(t) for t in self.tensors), n_pages, page)
         self.ref = ctypes.byref(self.desc)
 
@@ -395,7 +395,7 @@ class Chunks:
             raise ValueError("tok_off must have B + 1 entries and kv_len B")
         self.tensors = (tok_off, kv_len, block_table)
         self.device = _one_device(*self.tensors)
-        self.n_tokens = int(n_tokens)
+        self.dev, self.n_tokens = self.device.index, int(n_tokens)
         self.desc = ChunksDesc(batch, self.n_tokens, *(_dev_ptr(t) for t in self.tensors),
                                max_pages, int(max_chunk), int(max_kv))
         self.ref = ctypes.byref(self.desc)
@@ -408,55 +408,62 @@ def _one_device(*tensors):
     return devices.pop()
 
 
-class _on:
-    """The current device is `device` inside, whatever it was: a call's stream and
-    kernels are of the device that its tensors are on."""
+# A call of a decode step is a few microseconds of GPU work, so the checks below look at each
+# tensor once and take the stream as a number (torch's Stream object costs 2.6 us a call).
+_T = None
 
-    def __init__(self, device):
+
+def _torch():
+    global _T
+    if _T is None:
         import torch
-        self._guard = (None if device.index == torch.cuda.current_device()
-                       else torch.cuda.device(device))
-
-    def __enter__(self):
-        if self._guard is not None:
-            self._guard.__enter__()
-
-    def __exit__(self, *exc):
-        if self._guard is not None:
-            self._guard.__exit__(*exc)
+        _T = torch
+    return _T
 
 
-_ACT = {}
+def _run(fn, dev: int, stream, *args):
+    """fn(*args, stream) with `dev`, the device that the tensors are on, as the current one:
+    its stream and kernels are of that device, whatever the program's current device is."""
+    t = _torch()
+    if t._C._cuda_getDevice() != dev:
+        with t.cuda.device(dev):
+            return _run(fn, dev, stream, *args)
+    s = t._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    status = fn(*args, s)
+    if status != C2KV_OK:
+        _check(status)
 
 
-def _rows(t, cfg: AttnCfg, heads: int, n: int, device, what: str):
+def _act(cfg: AttnCfg):
+    return _torch().float32 if cfg.act_dtype == C2KV_F32 else _torch().bfloat16
+
+
+def _rows(t, cfg: AttnCfg, heads: int, n: int, dev: int, what: str):
     """Pointer and token stride of rows [n][heads][D]: tokens may lie apart, a token is dense."""
-    if not _ACT:
-        import torch
-        _ACT.update({C2KV_F32: torch.float32, C2KV_BF16: torch.bfloat16})
-    if t.dim() != 3 or t.shape[0] < n or t.shape[1] != heads or t.shape[2] != cfg.head_dim:
-        raise ValueError(f"{what} must be [{n}][{heads}][{cfg.head_dim}], got {list(t.shape)}")
-    if t.dtype is not _ACT.get(cfg.act_dtype) or t.device != device:
-        raise ValueError(f"{what} must have the act dtype and lie on {device}, "
+    shape, d = t.shape, cfg.head_dim
+    if len(shape) != 3 or shape[0] < n or shape[1] != heads or shape[2] != d:
+        raise ValueError(f"{what} must be [{n}][{heads}][{d}], got {list(shape)}")
+    if t.dtype is not _act(cfg) or t.get_device() != dev:
+        raise ValueError(f"{what} must have the act dtype and lie on device {dev}, "
                          f"got {t.dtype} on {t.device}")
     s0, s1, s2 = t.stride()
-    if s2 != 1 or s1 != cfg.head_dim and heads > 1:
+    if s2 != 1 or (s1 != d and heads > 1):
         raise ValueError(f"the heads of {what} must be dense")
-    return t.data_ptr(), s0 if t.shape[0] > 1 else 0
+    return t.data_ptr(), s0 if shape[0] > 1 else 0
 
 
-def _dense(t, cfg: AttnCfg, heads: int, n: int, device, what: str):
+def _dense(t, cfg: AttnCfg, heads: int, n: int, dev: int, what: str):
     if not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous")
-    return _rows(t, cfg, heads, n, device, what)[0]
+    return _rows(t, cfg, heads, n, dev, what)[0]
 
 
-def _index(t, dtype, n: int, device, what: str):
+def _index(t, dtype, n: int, dev: int, what: str):
     if t is None:
         return None
-    if t.dtype != dtype or t.dim() != 1 or t.shape[0] < n or t.device != device \
+    if t.dtype is not dtype or t.dim() != 1 or t.shape[0] < n or t.get_device() != dev \
             or not t.is_contiguous():
-        raise ValueError(f"{what} must be {dtype} [{n}], contiguous, on {device}")
+        raise ValueError(f"{what} must be {dtype} [{n}], contiguous, on device {dev}")
     return t.data_ptr()
 
 
@@ -464,44 +471,38 @@ def _of(cfg: AttnCfg, cache: Cache, chunks: Chunks):
     if cache.heads != cfg.n_kv_heads or cache.head_dim != cfg.head_dim:
         raise ValueError(f"the cache has {cache.heads} heads of {cache.head_dim}, the shape "
                          f"{cfg.n_kv_heads} of {cfg.head_dim}")
-    if cache.device != chunks.device:
+    if cache.dev != chunks.dev:
         raise ValueError(f"cache on {cache.device}, chunks on {chunks.device}")
-    return cache.device, chunks.n_tokens
+    return cache.dev, chunks.n_tokens
 
 
 def c2kv_cache_write(cfg: AttnCfg, cache: Cache, chunks: Chunks, k, v, pos=None, stream=None):
     """Put the chunks' tokens into the cache; pos [n_tokens] int32: k is turned to these
     positions (None: written as it is)."""
-    import torch
     dev, n = _of(cfg, cache, chunks)
     kp, ks = _rows(k, cfg, cfg.n_kv_heads, n, dev, "k")
     vp, vs = _rows(v, cfg, cfg.n_kv_heads, n, dev, "v")
-    pos = _index(pos, torch.int32, n, dev, "pos")
-    with _on(dev):
-        _check(_lib.c2kv_cache_write(ctypes.byref(cfg), cache.ref, chunks.ref, kp, ks, vp, vs,
-                                     pos, _stream(stream)))
+    pos = _index(pos, _T.int32, n, dev, "pos")
+    _run(_lib.c2kv_cache_write, dev, stream, ctypes.byref(cfg), cache.ref, chunks.ref, kp, ks, vp,
+         vs, pos)
 
 
 def c2kv_cache_read(cfg: AttnCfg, cache: Cache, chunks: Chunks, k, v, turn=None, stream=None):
     """The chunks' tokens as rows k and v [n_tokens][H_kv][D]; turn [n_tokens] int32 turns
     key i by turn[i] positions."""
-    import torch
     dev, n = _of(cfg, cache, chunks)
     kp = _dense(k, cfg, cfg.n_kv_heads, n, dev, "k")
     vp = _dense(v, cfg, cfg.n_kv_heads, n, dev, "v")
-    turn = _index(turn, torch.int32, n, dev, "turn")
-    with _on(dev):
-        _check(_lib.c2kv_cache_read(ctypes.byref(cfg), cache.ref, chunks.ref, turn, kp, vp,
-                                    _stream(stream)))
+    turn = _index(turn, _T.int32, n, dev, "turn")
+    _run(_lib.c2kv_cache_read, dev, stream, ctypes.byref(cfg), cache.ref, chunks.ref, turn, kp, vp)
 
 
 def cache_attend_workspace(cfg: AttnCfg, cache: Cache, chunks: Chunks):
     """A workspace for c2kv_cache_attend calls of this shape that are ordered."""
-    import torch
     nbytes = ctypes.c_size_t()
     _check(_lib.c2kv_cache_attend_workspace(ctypes.byref(cfg), cache.ref, chunks.ref,
                                             ctypes.byref(nbytes)))
-    raw = torch.empty(nbytes.value + 256, dtype=torch.uint8, device=cache.device)
+    raw = _torch().empty(nbytes.value + 256, dtype=_T.uint8, device=cache.device)
     off = (-raw.data_ptr()) % 256
     return raw[off:off + nbytes.value]
 
@@ -511,48 +512,43 @@ def c2kv_cache_attend(cfg: AttnCfg, cache: Cache, chunks: Chunks, q, out, pos=No
     """Causal attention of the chunks' queries over their requests' caches; pos [n_tokens]
     int32 turns q (None: as it is); lse [n_tokens][H_q] float32; workspace: from
     cache_attend_workspace (allocated for the call, on the current stream, if not given)."""
-    import torch
     dev, n = _of(cfg, cache, chunks)
     qp, qs = _rows(q, cfg, cfg.n_q_heads, n, dev, "q")
     op = _dense(out, cfg, cfg.n_q_heads, n, dev, "out")
-    pos = _index(pos, torch.int32, n, dev, "pos")
-    if lse is not None and (lse.dtype != torch.float32 or lse.device != dev or
-                            not lse.is_contiguous() or lse.dim() != 2 or lse.shape[0] < n or
-                            lse.shape[1] != cfg.n_q_heads):
-        raise ValueError(f"lse must be float32 [{n}][{cfg.n_q_heads}], contiguous, on {dev}")
-    with _on(dev):
-        if workspace is None:
-            if stream is not None:
-                raise ValueError("a call on another stream needs a workspace of its own")
-            workspace = cache_attend_workspace(cfg, cache, chunks)
-        elif workspace.device != dev or not workspace.is_contiguous():
-            raise ValueError(f"workspace must be contiguous and lie on {dev}")
-        _check(_lib.c2kv_cache_attend(ctypes.byref(cfg), cache.ref, chunks.ref, qp, qs, pos, op,
-                                      None if lse is None else lse.data_ptr(),
-                                      workspace.data_ptr(),
-                                      workspace.numel() * workspace.element_size(),
-                                      _stream(stream)))
+    pos = _index(pos, _T.int32, n, dev, "pos")
+    if lse is not None:
+        if lse.dtype is not _T.float32 or lse.get_device() != dev or lse.dim() != 2 or \
+                lse.shape[0] < n or lse.shape[1] != cfg.n_q_heads or not lse.is_contiguous():
+            raise ValueError(f"lse must be float32 [{n}][{cfg.n_q_heads}], contiguous, on "
+                             f"device {dev}")
+        lse = lse.data_ptr()
+    if workspace is None:
+        if stream is not None:
+            raise ValueError("a call on another stream needs a workspace of its own")
+        workspace = cache_attend_workspace(cfg, cache, chunks)
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous and lie on device {dev}")
+    _run(_lib.c2kv_cache_attend, dev, stream, ctypes.byref(cfg), cache.ref, chunks.ref, qp, qs,
+         pos, op, lse, workspace.data_ptr(), workspace.nbytes)
 
 
 def c2kv_pool_write(cfg: AttnCfg, pool: PoolDesc, row, k, v, pos=None, stream=None):
     """Store the rows k and v [n][H_kv][D] in pool rows row [n] int64, quantised as they are
     written where the pool is int8; pos [n] int32 encodes k at these positions."""
-    import torch
-    n, dev = int(row.shape[0]), row.device
-    rows = _index(row, torch.int64, n, dev, "row")
-    if not row.is_cuda:
+    n, dev = row.shape[0], row.get_device()
+    if dev < 0:
         raise ValueError("expected a device tensor")
+    rows = _index(row, _torch().int64, n, dev, "row")
     if getattr(pool, "row_shape", None) not in (None, (cfg.n_kv_heads, cfg.head_dim)):
         raise ValueError(f"the pool's rows are {pool.row_shape}, the shape has "
                          f"{(cfg.n_kv_heads, cfg.head_dim)}")
-    if getattr(pool, "device", dev) != dev:
-        raise ValueError(f"pool on {pool.device}, rows on {dev}")
+    if getattr(pool, "dev", dev) != dev:
+        raise ValueError(f"pool on device {pool.dev}, rows on {dev}")
     kp, ks = _rows(k, cfg, cfg.n_kv_heads, n, dev, "k")
     vp, vs = _rows(v, cfg, cfg.n_kv_heads, n, dev, "v")
-    pos = _index(pos, torch.int32, n, dev, "pos")
-    with _on(dev):
-        _check(_lib.c2kv_pool_write(ctypes.byref(cfg), ctypes.byref(pool), n, rows, kp, ks, vp,
-                                    vs, pos, _stream(stream)))
+    pos = _index(pos, _T.int32, n, dev, "pos")
+    _run(_lib.c2kv_pool_write, dev, stream, ctypes.byref(cfg), ctypes.byref(pool), n, rows, kp, ks,
+         vp, vs, pos)
 
 
 class HostPool:

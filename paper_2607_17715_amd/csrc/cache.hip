@@ -73,48 +73,53 @@ __device__ inline void stream8(__bf16* p, const float (&x)[8]) {
 // RoPE and int8
 // ----------------------------------------------------------------------------
 
-// Largest magnitude as bits, NaN above all: a row that holds one gets a NaN scale, and
-// reads back as NaN.
-__device__ inline uint32_t mag(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+// Largest magnitude of what has been seen; a NaN stays.
+__device__ inline float max_mag(float m, float x, float y) {
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(m, __builtin_fabsf(x)),
+                                       __builtin_fabsf(y));
+}
 // its maximum over groups of LANES neighbouring lanes, by lane moves inside the VALU up to 16
 template <int CTRL>
-__device__ inline uint32_t max_with(uint32_t m) {
-  return max(m, uint32_t(__builtin_amdgcn_update_dpp(0, int(m), CTRL, 0xf, 0xf, true)));
+__device__ inline float max_with(float m) {
+  return __builtin_elementwise_maximum(
+      m, __uint_as_float(__builtin_amdgcn_update_dpp(0, int(__float_as_uint(m)), CTRL, 0xf, 0xf,
+                                                     true)));
 }
 template <int LANES>
-__device__ inline uint32_t lanes_max(uint32_t m) {
+__device__ inline float lanes_max(float m) {
   m = max_with<0xb1>(m);                      // lane ^ 1
   m = max_with<0x4e>(m);                      // lane ^ 2
   if constexpr (LANES >= 8) m = max_with<0x141>(m);    // the other four of eight (mirrored)
   if constexpr (LANES >= 16) m = max_with<0x140>(m);   // the other eight of sixteen
 #pragma unroll
-  for (int d = 16; d < LANES; d *= 2) m = max(m, uint32_t(__shfl_xor(int(m), d)));
+  for (int d = 16; d < LANES; d *= 2) m = __builtin_elementwise_maximum(m, __shfl_xor(m, d));
   return m;
 }
 
-// Symmetric int8 of a row with the largest magnitude m (as bits): scale = m / 127, code =
-// x / scale to the nearest, ties to even.  A quotient is a product with the reciprocal and
-// one correction by its remainder, what a division does without the cases that cannot
-// occur here (write of 16384 tokens: 41 -> 32 us, where a full division an element was the
-// bound); no |quotient| passes 127.5, so nothing is clamped.  A row below 2^-100, whose
-// reciprocal would leave the range, is stored as zeros; one with an infinity or a NaN gets a
-// NaN scale, whatever its codes.
+// Symmetric int8 of a row whose largest magnitude is m: scale = m / 127, code = x / scale to
+// the nearest.  An element costs one fused multiply-add: its product with the scale's
+// reciprocal (within 2^-23, so that a quotient that near to a half may go either way) is
+// added to 1.5 * 2^23, which rounds it to a whole number, in the low bits of the sum in
+// two's complement.  No |quotient| passes 127.5, so nothing is clamped.  (A full division an
+// element was the bound of these kernels: 16384 tokens written in 41 us, 32 without, both
+// before their stores streamed.)  A row below 2^-100, whose reciprocal would leave the
+// range, is stored as zeros; one with an infinity or a NaN gets a NaN scale, whatever its
+// codes.
 struct I8Row {
   float scale, inv;
-  __device__ explicit I8Row(uint32_t m) {
-    const float x = __uint_as_float(m), c = 1.f / 127.f;
-    float s = x * c;
-    s = __builtin_fmaf(__builtin_fmaf(-s, 127.f, x), c, s);
-    const bool tiny = m < 0x0d800000u;                    // 2^-100
-    scale = m >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : tiny ? 1.f : s;
-    inv = tiny ? 0.f : __builtin_amdgcn_rcpf(s);
+  __device__ explicit I8Row(float m) {
+    const float c = 1.f / 127.f;
+    float s = m * c;
+    s = __builtin_fmaf(__builtin_fmaf(-s, 127.f, m), c, s);      // correctly rounded
+    float r = __builtin_amdgcn_rcpf(s);
+    r = __builtin_fmaf(__builtin_fmaf(-s, r, 1.f), r, r);
+    const bool tiny = m < 0x1p-100f;
+    scale = m < __builtin_huge_valf() ? (tiny ? 1.f : s) : __builtin_nanf("");
+    inv = tiny ? 0.f : r;
   }
-  // the code as the low byte of a word: added to 1.5 * 2^23 the quotient is rounded to a
-  // whole number, in the low bits of the sum in two's complement
+  // the code as the low byte of a word
   __device__ uint32_t code(float x) const {
-    float q = x * inv;
-    q = __builtin_fmaf(__builtin_fmaf(-q, scale, x), inv, q);
-    return __float_as_uint(q + 12582912.f);
+    return __float_as_uint(__builtin_fmaf(x, inv, 12582912.f));
   }
   __device__ uint32_t pack4(const float* x) const {
     const uint32_t lo = __builtin_amdgcn_perm(code(x[1]), code(x[0]), 0x0c0c0400u);
@@ -196,10 +201,8 @@ __global__ __launch_bounds__(256) void write_rows_kernel(WriteParams a) {
   S* kp = static_cast<S*>(a.pg.k) + (ph * a.pg.PS + off) * D;
   S* vp = static_cast<S*>(a.pg.v) + ph * D * a.pg.PS + off;
   if constexpr (sizeof(S) == 1) {
-    uint32_t mv = mag(v[0]);
-#pragma unroll
-    for (int e = 1; e < VPL; ++e) mv = max(mv, mag(v[e]));
-    const I8Row ks(lanes_max<64>(max(mag(x), mag(y)))), vs(lanes_max<64>(mv));
+    const I8Row ks(lanes_max<64>(max_mag(0.f, x, y)));
+    const I8Row vs(lanes_max<64>(max_mag(0.f, v[0], v[VPL - 1])));
     if (lane == 0) {
       a.pg.k_scale[ph * a.pg.PS + off] = ks.scale;
       a.pg.v_scale[ph * a.pg.PS + off] = vs.scale;
@@ -280,10 +283,10 @@ __global__ __launch_bounds__(256) void write_tile_kernel(WriteParams a) {
       const int u = tid + i * NTH;
       const int slot = u / KU, c = u % KU;
       if (a.rope.pos) rotate8(x[i], y[i], kc[i], kn[i]);
-      uint32_t m = 0;
+      float m = 0.f;
       if constexpr (sizeof(S) == 1) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) m = max(m, max(mag(x[i][e]), mag(y[i][e])));
+        for (int e = 0; e < 8; ++e) m = max_mag(m, x[i][e], y[i][e]);
         m = lanes_max<KU>(m);
       }
       const I8Row q(m);
@@ -298,12 +301,12 @@ __global__ __launch_bounds__(256) void write_tile_kernel(WriteParams a) {
     for (int i = 0; i < NVU; ++i) {
       const int u = tid + i * NTH;
       const int slot = 2 * (u / VU), c = u % VU;
-      uint32_t m[2] = {0, 0};
+      float m[2] = {0.f, 0.f};
       if constexpr (sizeof(S) == 1) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) m[j] = max(m[j], mag(v[i][j][e]));
+          for (int e = 0; e < 8; e += 2) m[j] = max_mag(m[j], v[i][j][e], v[i][j][e + 1]);
           m[j] = lanes_max<VU>(m[j]);
         }
       }
@@ -481,12 +484,12 @@ __global__ __launch_bounds__(256) void pool_write_kernel(PoolWriteParams a) {
     load8(v, x[1]);
     load8(v + D / 2, y[1]);
     if (a.rope.pos) rotate8(x[0], y[0], kc, kn);
-    uint32_t m[2] = {0, 0};
+    float m[2] = {0.f, 0.f};
     if constexpr (sizeof(S) == 1) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) m[j] = max(m[j], max(mag(x[j][e]), mag(y[j][e])));
+        for (int e = 0; e < 8; ++e) m[j] = max_mag(m[j], x[j][e], y[j][e]);
         m[j] = lanes_max<KU>(m[j]);
       }
     }

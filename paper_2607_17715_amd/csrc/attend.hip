@@ -58,6 +58,34 @@ struct Share {
   unsigned p0, p1;
 };
 
+// head_tiles of a request that all lanes name, its row blocks dealt to the lanes.
+template <int RB>
+__device__ inline unsigned head_tiles_wave(const Req& r, unsigned G, int limit) {
+  const int lane = threadIdx.x & 63, n = row_blocks(r, G, RB);
+  unsigned t = 0;
+  for (int i = lane; i < n; i += 64) t += unsigned(unit_tiles(r, G, RB, i, limit));
+  return unsigned(__builtin_amdgcn_readlane(int(wave_scan(t)), 63));
+}
+// The row block of r in which tile `rest` of a kv-head lies; rest becomes the tile in it.
+template <int RB>
+__device__ inline int find_block(const Req& r, unsigned G, int limit, unsigned& rest, int& tiles) {
+  const int lane = threadIdx.x & 63, n = row_blocks(r, G, RB);
+  for (int i0 = 0; i0 < n; i0 += 64) {
+    const unsigned t = i0 + lane < n ? unsigned(unit_tiles(r, G, RB, i0 + lane, limit)) : 0;
+    const unsigned incl = wave_scan(t);
+    const unsigned here = unsigned(__builtin_amdgcn_readlane(int(incl), 63));
+    if (rest < here) {
+      const int src = __builtin_ctzll(__ballot(incl > rest));
+      tiles = __builtin_amdgcn_readlane(int(t), src);
+      rest -= unsigned(__builtin_amdgcn_readlane(int(incl - t), src));
+      return i0 + src;
+    }
+    rest -= here;
+  }
+  tiles = 1;                                 // (not reached: rest is below head_tiles)
+  return max(n - 1, 0);
+}
+
 template <int RB>
 __device__ inline Share find_share(const AttendParams& a, int w, int limit, unsigned least,
                                    Place& at) {
@@ -68,7 +96,23 @@ __device__ inline Share find_share(const AttendParams& a, int w, int limit, unsi
   auto step = [&](int b0) {
     const int b = b0 + lane;
     mine = request(a.ch, min(b, a.ch.batch - 1));
-    head = b < a.ch.batch ? head_tiles(mine, a.G, RB, limit) : 0;
+    // row blocks lane by lane, a request each; few requests of many blocks one by one, their
+    // blocks dealt to the lanes (one of 64: 6000 cycles against 400)
+    const int blocks = b < a.ch.batch ? row_blocks(mine, a.G, RB) : 0;
+    uint64_t some = __ballot(blocks > 0);
+    if (__any(blocks > 4 * __builtin_popcountll(some))) {
+      head = 0;
+      for (; some; some &= some - 1) {
+        const int src = __builtin_ctzll(some);
+        const Req r = {__builtin_amdgcn_readlane(mine.first, src),
+                       __builtin_amdgcn_readlane(mine.n, src),
+                       __builtin_amdgcn_readlane(mine.base, src)};
+        const unsigned t = head_tiles_wave<RB>(r, a.G, limit);
+        if (lane == src) head = t;
+      }
+    } else {
+      head = blocks > 0 ? head_tiles(mine, a.G, RB, limit) : 0;
+    }
     cost = head * a.pg.Hkv;
     incl = wave_scan(cost);
     return unsigned(__builtin_amdgcn_readlane(int(incl), 63));
@@ -92,10 +136,7 @@ __device__ inline Share find_share(const AttendParams& a, int w, int limit, unsi
       unsigned rest = s.p0 - seen - (of(incl) - of(cost));
       at.g = int(rest / of(head));
       rest -= at.g * of(head);
-      UnitWalk u(at.r, a.G, RB, limit);
-      at.i = 0;
-      for (; rest >= unsigned(u.tiles()); u.next(), ++at.i) rest -= u.tiles();
-      at.tiles = u.tiles();
+      at.i = find_block<RB>(at.r, a.G, limit, rest, at.tiles);
       at.tile = int(rest);
       return s;
     }
@@ -613,8 +654,11 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
                     (NTH / W::CV) % (W::MV + 1) == 0,
                 "a thread's chunks of one tile lie in rows of one permutation");
 
-  constexpr int XW = 2 + 16 * NDB;               // what key parts exchange: floats a lane
-  constexpr int XBYTES = KG == 2 ? RG * 64 * XW * 4 : 0;
+  // After the tiles the stages serve the key parts' exchange (XW floats a lane) and the way
+  // of the rows out (OUT bytes a wavefront).
+  constexpr int XW = 4 + 16 * NDB, OUT = 32 * 64 * 4;
+  constexpr int XBYTES = KG == 2 ? RG * 64 * XW * 4 : 8 * OUT;
+  static_assert(KG == 1 || 64 * XW * 4 >= OUT, "a row group's exchange holds its rows' way out");
   __shared__ __attribute__((aligned(1024)))
   uint8_t lds[NST * W::BYTES > XBYTES ? NST * W::BYTES : XBYTES];
   __shared__ double s_turns[D / 2];
@@ -673,35 +717,31 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
     // keys of a tile that exist
     auto there = [&](int tile, int page) { return page < 0 ? 0 : min(max(keys - tile * ST, 0), ST); };
 
-    // int8: BPT codes of a key (elements kd ..) and of a value row (keys vk ..) a thread
+    // int8: BPT codes of a key (elements ikd ..) and of a value row (keys ivk ..) a thread.
+    // Lane l has the value scale of key l, and a value row's keys of its own group of 16.
     constexpr int BPT = ST * D / NTH;
     const int ikey = tid / (D / BPT), ikd = tid % (D / BPT) * BPT;
-    const int ivd = tid / (ST / BPT), ivk = tid % (ST / BPT) * BPT;
+    const int ivd = wave * BPT + lane % BPT, ivk = lane / BPT * BPT;
     uint32_t kraw[BPT / 4], vraw[BPT / 4];
-    float kscale = 0.f, vscale[BPT];
+    float kscale = 0.f, vscale = 0.f;
     auto load_i8 = [&](int tile) __attribute__((always_inline)) {
       const int page = max(page_id(tile), 0), off = tile * ST % PS;
       const size_t ph = size_t(page) * a.pg.Hkv + at.g;
       const int8_t* kp = static_cast<const int8_t*>(a.pg.k) + (ph * PS + off + ikey) * D + ikd;
       const int8_t* vp = static_cast<const int8_t*>(a.pg.v) + (ph * D + ivd) * PS + off + ivk;
-      const float* sp = a.pg.v_scale + ph * PS + off + ivk;
 #pragma unroll
       for (int i = 0; i < BPT / 8; ++i) {
         raw_load8<int8_t>(kraw + 2 * i, kp + 8 * i);
         raw_load8<int8_t>(vraw + 2 * i, vp + 8 * i);
-        float x[8];
-        load8(sp + 8 * i, x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) vscale[8 * i + e] = x[e];
       }
+      vscale = a.pg.v_scale[ph * PS + off + lane];
       kscale = a.pg.k_scale[ph * PS + off + ikey];
     };
     auto commit_i8 = [&](int tile) __attribute__((always_inline)) {
       const int n = there(tile, page_id(tile));
-      if (n < ST) {                              // (a scale behind the last key may be anything)
-#pragma unroll
-        for (int e = 0; e < BPT; ++e) vscale[e] = ivk + e < n ? vscale[e] : 0.f;
-      }
+      // (a scale behind the last key may be anything)
+      float vs[16];
+      lanes16(lane < n ? vscale : 0.f, vs, std::make_integer_sequence<int, 16>{});
       uint8_t* st = stage(tile);
 #pragma unroll
       for (int i = 0; i < BPT / 8; ++i) {
@@ -711,7 +751,7 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           x[e] *= kscale;
-          y[e] *= vscale[8 * i + e];
+          y[e] *= BPT == 16 ? vs[8 * i + e] : lane & 8 ? vs[8 + e] : vs[e];
         }
         *reinterpret_cast<bf16x8*>(st + W::k_at(ikey, ikd / 8 + i)) = bf16_of(x);
         *reinterpret_cast<bf16x8*>(st + W::v_at(ivd, ivk / 8 + i)) = bf16_of(y);
@@ -960,61 +1000,105 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
     }
 
     // ---- the key parts of a row group meet
+    lds_barrier();                               // the tiles are read
     float l_tot = half_pair_sum(l_run);
     if constexpr (KG == 2) {
-      lds_barrier();
       float* mine = reinterpret_cast<float*>(lds) + (rg * 64 + lane) * XW;
       if (kg == 1) {
-        mine[0] = m_run;
-        mine[1] = l_tot;
+        *reinterpret_cast<float2*>(mine) = make_float2(m_run, l_tot);
 #pragma unroll
-        for (int i = 0; i < 16 * NDB; ++i) mine[2 + i] = o[i / 16][i % 16];
+        for (int i = 0; i < 4 * NDB; ++i) {
+          const int v = 4 * (i % 4);
+          const f32x16& b = o[i / 4];
+          *reinterpret_cast<float4*>(mine + 4 + 4 * i) =
+              make_float4(b[v], b[v + 1], b[v + 2], b[v + 3]);
+        }
       }
       lds_barrier();
       if (kg == 0) {
-        const float m = fmaxf(m_run, mine[0]), ref = m == kNegInf ? 0.f : m;
+        const float2 ml = *reinterpret_cast<const float2*>(mine);
+        const float m = fmaxf(m_run, ml.x), ref = m == kNegInf ? 0.f : m;
         const float f0 = __builtin_amdgcn_exp2f(m_run - ref);
-        const float f1 = __builtin_amdgcn_exp2f(mine[0] - ref);
-        l_tot = l_tot * f0 + mine[1] * f1;
+        const float f1 = __builtin_amdgcn_exp2f(ml.x - ref);
+        l_tot = l_tot * f0 + ml.y * f1;
         m_run = m;
 #pragma unroll
-        for (int i = 0; i < 16 * NDB; ++i)
-          o[i / 16][i % 16] = o[i / 16][i % 16] * f0 + mine[2 + i] * f1;
+        for (int i = 0; i < 4 * NDB; ++i) {
+          const float4 x = *reinterpret_cast<const float4*>(mine + 4 + 4 * i);
+          const float xs[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            o[i / 4][4 * (i % 4) + e] = o[i / 4][4 * (i % 4) + e] * f0 + xs[e] * f1;
+        }
       }
     }
-    const bool begins = cur.begins(), ends = cur.ends();
+
+    // ---- the rows leave, 64 columns at a time, through LDS of the wavefront's own, so that a
+    // store writes whole lines (a lane's own values are 16 bytes of each of 32 rows: 8000
+    // cycles a unit of 256 rows).  Values 4 i .. 4 i + 3 of block db are elements 32 db + 8 i +
+    // 4 half + 0 .. 3; a row's 16-byte chunks are permuted by its index.
+    const bool begins = cur.begins(), ends = cur.ends(), whole = begins && ends;
     if (begins && !ends) join = cur.cut(share);
-    if (kg == 0 && 32 * rg + col < nrows) {
+    if (kg == 0 && rows_here) {
       const float ref = m_run == kNegInf ? 0.f : m_run;
-      // values 4 i .. 4 i + 3 of block db are elements 32 db + 8 i + 4 half + 0 .. 3
-      if (begins && ends) {
-        const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;
-        const size_t oh = size_t(at.r.first + t) * a.Hq + at.g * a.G + row % a.G;
-        T* out = static_cast<T*>(a.out) + oh * D + 4 * half;
+      const float inv = !whole ? 1.f : l_tot == 0.f ? 0.f : 1.f / l_tot;
+      uint8_t* way = lds + (KG == 2 ? rg * 64 * XW * 4 : wave * OUT);
+      const int rows = min(32, nrows - 32 * rg);
+      if (half == 0 && col < rows) {
+        if (!whole)
+          a.part_ml[(size_t(2) * w + (begins ? 1 : 0)) * RB + 32 * rg + col] =
+              make_float2(m_run, l_tot);
+        else if (a.lse)
+          a.lse[size_t(at.r.first + int(t)) * a.Hq + at.g * a.G + row % a.G] =
+              l_tot == 0.f ? kNegInf : (ref + __builtin_amdgcn_logf(l_tot)) * kLn2;
+      }
 #pragma unroll
-        for (int i = 0; i < 4 * NDB; ++i) {
-          const f32x16& b = o[i / 4];
-          const int v = 4 * (i % 4);
-          if constexpr (F32)
-            *reinterpret_cast<float4*>(out + 8 * i) =
-                make_float4(b[v] * inv, b[v + 1] * inv, b[v + 2] * inv, b[v + 3] * inv);
-          else
-            *reinterpret_cast<uint2*>(out + 8 * i) =
-                make_uint2(pack_bf16(b[v] * inv, b[v + 1] * inv),
-                           pack_bf16(b[v + 2] * inv, b[v + 3] * inv));
-        }
-        if (a.lse && half == 0)
-          a.lse[oh] = l_tot == 0.f ? kNegInf : (ref + __builtin_amdgcn_logf(l_tot)) * kLn2;
-      } else {
-        const size_t part = (size_t(2) * w + (begins ? 1 : 0)) * RB + 32 * rg + col;
-        float* to = a.part_o + part * D + 4 * half;
+      for (int d0 = 0; d0 < D; d0 += 64) {
 #pragma unroll
-        for (int i = 0; i < 4 * NDB; ++i) {
-          const f32x16& b = o[i / 4];
+        for (int i = 0; i < 8; ++i) {
+          const f32x16& b = o[d0 / 32 + i / 4];
           const int v = 4 * (i % 4);
-          *reinterpret_cast<float4*>(to + 8 * i) = make_float4(b[v], b[v + 1], b[v + 2], b[v + 3]);
+          *reinterpret_cast<float4*>(way + col * 256 + ((2 * i + half) ^ (col & 15)) * 16) =
+              make_float4(b[v] * inv, b[v + 1] * inv, b[v + 2] * inv, b[v + 3] * inv);
         }
-        if (half == 0) a.part_ml[part] = make_float2(m_run, l_tot);
+        // (the wavefront's LDS accesses are in order)
+        __builtin_amdgcn_wave_barrier();
+        constexpr int CPR = 16;                  // chunks of four elements
+        if (F32 || !whole) {
+#pragma unroll
+          for (int i = 0; i < 32 * CPR / 64; ++i) {
+            const int r = (i * 64 + lane) / CPR, c = lane % CPR;
+            const float4 x =
+                *reinterpret_cast<const float4*>(way + r * 256 + (c ^ (r & 15)) * 16);
+            if (r >= rows) continue;
+            const int rr = row0 + 32 * rg + r;
+            float* to;
+            if (!whole) {
+              to = a.part_o + ((size_t(2) * w + (begins ? 1 : 0)) * RB + 32 * rg + r) * D;
+            } else {
+              const unsigned tk = unsigned(rr) / unsigned(a.G);
+              to = static_cast<float*>(a.out) +
+                   (size_t(at.r.first + int(tk)) * a.Hq + at.g * a.G + (rr - tk * a.G)) * D;
+            }
+            *reinterpret_cast<float4*>(to + d0 + 4 * c) = x;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32 * CPR / 2 / 64; ++i) {
+            const int r = (i * 64 + lane) / (CPR / 2), c = 2 * (lane % (CPR / 2));
+            const uint8_t* from = way + r * 256;
+            const float4 x = *reinterpret_cast<const float4*>(from + (c ^ (r & 15)) * 16);
+            const float4 y = *reinterpret_cast<const float4*>(from + ((c + 1) ^ (r & 15)) * 16);
+            if (r >= rows) continue;
+            const unsigned rr = row0 + 32 * rg + r, tk = rr / unsigned(a.G);
+            T* to = static_cast<T*>(a.out) +
+                    (size_t(at.r.first + int(tk)) * a.Hq + at.g * a.G + (rr - tk * a.G)) * D;
+            *reinterpret_cast<uint4*>(to + d0 + 4 * c) =
+                make_uint4(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w), pack_bf16(y.x, y.y),
+                           pack_bf16(y.z, y.w));
+          }
+        }
+        __builtin_amdgcn_wave_barrier();
       }
     }
     p += t1 - t0;

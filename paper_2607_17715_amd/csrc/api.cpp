@@ -231,10 +231,14 @@ int longest_chunk(const c2kv_chunks& c) {
 // Launch shape of an attention call, from the bounds that the host knows.
 c2kv::AttendShape attend_shape(const c2kv_attn_cfg& cfg, const c2kv_cache& cache,
                                const c2kv_chunks& ch) {
-  const int64_t G = cfg.n_q_heads / cfg.n_kv_heads, longest = longest_chunk(ch);
+  const int64_t G = cfg.n_q_heads / cfg.n_kv_heads;
+  // (as many rows as requests: most likely one token each)
+  const int64_t longest = ch.max_chunk == 0 && ch.n_tokens <= ch.batch ? 1
+                          : ch.n_tokens < 1                            ? 1
+                                                                       : longest_chunk(ch);
   const int64_t room = int64_t(ch.max_pages) * cache.page_size;
   const int64_t kv = ch.max_kv > 0 && ch.max_kv < room ? ch.max_kv : room;
-  return c2kv::attend_shape(cache.dtype, cfg.head_dim, longest * G, ch.batch,
+  return c2kv::attend_shape(cache.dtype, cfg.head_dim, longest * G, longest, ch.batch,
                             cfg.n_kv_heads, kv);
 }
 
@@ -242,7 +246,7 @@ c2kv::AttendShape attend_shape(const c2kv_attn_cfg& cfg, const c2kv_cache& cache
 bool too_long(const c2kv::AttendShape& sh, const c2kv_attn_cfg& cfg, const c2kv_cache& cache,
               const c2kv_chunks& ch) {
   return c2kv::most_tiles(ch.n_tokens, ch.batch, cfg.n_q_heads / cfg.n_kv_heads, cfg.n_kv_heads,
-                          sh.rows, int64_t(ch.max_pages) * cache.page_size) >= 1ll << 31;
+                          sh.unit_rows, int64_t(ch.max_pages) * cache.page_size) >= 1ll << 31;
 }
 const char kTooLong[] = "batches that may hold 2^31 key tiles are not built";
 
@@ -597,6 +601,7 @@ c2kv_status c2kv_cache_attend(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,
     p.rope = rope(*cfg, pos);
     p.Hq = cfg->n_q_heads;
     p.G = cfg->n_q_heads / cfg->n_kv_heads;
+    p.rb = sh.unit_rows;
     p.qscale = float(double(scale) * 1.4426950408889634074);
     p.q = q;
     p.q_stride = q_stride;

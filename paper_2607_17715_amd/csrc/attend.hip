@@ -1,7 +1,9 @@
 // Attention of chunks of new tokens over a growing paged cache, for gfx950 (CDNA4).
 //
-//   attend_narrow_kernel   few query rows a unit (single tokens, drafts): every wavefront
-//                          reads its own keys straight into MFMA operands
+//   attend_narrow_kernel   one token a unit: every wavefront reads its own keys straight
+//                          into MFMA operands
+//   attend_wide_kernel     blocks of 128 or 256 query rows: tiles in LDS, shared by the
+//                          wavefronts
 //   join_kernel            log-sum-exp combine of units that lie in several workgroups
 //
 // The work of a launch is one line of key tiles (cache_index.hpp), shared evenly by its
@@ -59,19 +61,18 @@ struct Share {
 };
 
 // head_tiles of a request that all lanes name, its row blocks dealt to the lanes.
-template <int RB>
-__device__ inline unsigned head_tiles_wave(const Req& r, unsigned G, int limit) {
-  const int lane = threadIdx.x & 63, n = row_blocks(r, G, RB);
+__device__ inline unsigned head_tiles_wave(const Req& r, unsigned G, int rb, int limit) {
+  const int lane = threadIdx.x & 63, n = row_blocks(r, G, rb);
   unsigned t = 0;
-  for (int i = lane; i < n; i += 64) t += unsigned(unit_tiles(r, G, RB, i, limit));
+  for (int i = lane; i < n; i += 64) t += unsigned(unit_tiles(r, G, rb, i, limit));
   return unsigned(__builtin_amdgcn_readlane(int(wave_scan(t)), 63));
 }
 // The row block of r in which tile `rest` of a kv-head lies; rest becomes the tile in it.
-template <int RB>
-__device__ inline int find_block(const Req& r, unsigned G, int limit, unsigned& rest, int& tiles) {
-  const int lane = threadIdx.x & 63, n = row_blocks(r, G, RB);
+__device__ inline int find_block(const Req& r, unsigned G, int rb, int limit, unsigned& rest,
+                                 int& tiles) {
+  const int lane = threadIdx.x & 63, n = row_blocks(r, G, rb);
   for (int i0 = 0; i0 < n; i0 += 64) {
-    const unsigned t = i0 + lane < n ? unsigned(unit_tiles(r, G, RB, i0 + lane, limit)) : 0;
+    const unsigned t = i0 + lane < n ? unsigned(unit_tiles(r, G, rb, i0 + lane, limit)) : 0;
     const unsigned incl = wave_scan(t);
     const unsigned here = unsigned(__builtin_amdgcn_readlane(int(incl), 63));
     if (rest < here) {
@@ -86,9 +87,8 @@ __device__ inline int find_block(const Req& r, unsigned G, int limit, unsigned& 
   return max(n - 1, 0);
 }
 
-template <int RB>
-__device__ inline Share find_share(const AttendParams& a, int w, int limit, unsigned least,
-                                   Place& at) {
+__device__ inline Share find_share(const AttendParams& a, int w, int rb, int limit,
+                                   unsigned least, Place& at) {
   const int lane = threadIdx.x & 63;
   Share s{};
   Req mine{};
@@ -98,7 +98,7 @@ __device__ inline Share find_share(const AttendParams& a, int w, int limit, unsi
     mine = request(a.ch, min(b, a.ch.batch - 1));
     // row blocks lane by lane, a request each; few requests of many blocks one by one, their
     // blocks dealt to the lanes (one of 64: 6000 cycles against 400)
-    const int blocks = b < a.ch.batch ? row_blocks(mine, a.G, RB) : 0;
+    const int blocks = b < a.ch.batch ? row_blocks(mine, a.G, rb) : 0;
     uint64_t some = __ballot(blocks > 0);
     if (__any(blocks > 4 * __builtin_popcountll(some))) {
       head = 0;
@@ -107,11 +107,11 @@ __device__ inline Share find_share(const AttendParams& a, int w, int limit, unsi
         const Req r = {__builtin_amdgcn_readlane(mine.first, src),
                        __builtin_amdgcn_readlane(mine.n, src),
                        __builtin_amdgcn_readlane(mine.base, src)};
-        const unsigned t = head_tiles_wave<RB>(r, a.G, limit);
+        const unsigned t = head_tiles_wave(r, a.G, rb, limit);
         if (lane == src) head = t;
       }
     } else {
-      head = blocks > 0 ? head_tiles(mine, a.G, RB, limit) : 0;
+      head = blocks > 0 ? head_tiles(mine, a.G, rb, limit) : 0;
     }
     cost = head * a.pg.Hkv;
     incl = wave_scan(cost);
@@ -136,7 +136,7 @@ __device__ inline Share find_share(const AttendParams& a, int w, int limit, unsi
       unsigned rest = s.p0 - seen - (of(incl) - of(cost));
       at.g = int(rest / of(head));
       rest -= at.g * of(head);
-      at.i = find_block<RB>(at.r, a.G, limit, rest, at.tiles);
+      at.i = find_block(at.r, a.G, rb, limit, rest, at.tiles);
       at.tile = int(rest);
       return s;
     }
@@ -146,9 +146,8 @@ __device__ inline Share find_share(const AttendParams& a, int w, int limit, unsi
 }
 
 // The unit after `at`, entered at its first tile.
-template <int RB>
-__device__ inline void next_unit(const AttendParams& a, int limit, Place& at) {
-  if (++at.i >= row_blocks(at.r, a.G, RB)) {
+__device__ inline void next_unit(const AttendParams& a, int rb, int limit, Place& at) {
+  if (++at.i >= row_blocks(at.r, a.G, rb)) {
     at.i = 0;
     if (++at.g >= a.pg.Hkv) {
       at.g = 0;
@@ -159,20 +158,19 @@ __device__ inline void next_unit(const AttendParams& a, int limit, Place& at) {
       } while (at.r.n == 0);
     }
   }
-  at.tiles = unit_tiles(at.r, a.G, RB, at.i, limit);
+  at.tiles = unit_tiles(at.r, a.G, rb, at.i, limit);
   at.tile = 0;
 }
 
 // The tiles [t0, t1) of a unit that a workgroup works on.
-template <int RB>
 struct Piece {
   Req r;
   int b, g, t0, t1, tiles, keys, row0, nrows;
-  __device__ Piece(const AttendParams& a, int limit, const Place& at, unsigned left)
+  __device__ Piece(const AttendParams& a, int rb, int limit, const Place& at, unsigned left)
       : r(at.r), b(at.b), g(at.g), t0(at.tile),
         t1(int(min(unsigned(at.tiles), at.tile + left))), tiles(at.tiles),
-        keys(unit_keys(at.r, a.G, RB, at.i, limit)), row0(at.i * RB),
-        nrows(min(RB, at.r.n * a.G - at.i * RB)) {}
+        keys(unit_keys(at.r, a.G, rb, at.i, limit)), row0(at.i * rb),
+        nrows(min(rb, at.r.n * a.G - at.i * rb)) {}
   __device__ bool begins() const { return t0 == 0; }
   __device__ bool ends() const { return t1 == tiles; }
   // the join of a unit that begins in this workgroup, whose share ends (at p1) inside it
@@ -241,12 +239,72 @@ __device__ inline void lanes16(float x, float (&v)[16], std::integer_sequence<in
                                                        0xf, 0xf, true))), ...);
 }
 
+// Values that are not finite, in tiles where some rows see a key and others do not: a
+// probability of zero times an infinity would put a NaN into rows that must not know of it.
+// Such elements are taken out of the product, and what they add to the rows that do see them
+// comes from products of the same probabilities with where they are: an infinity, or, where
+// both signs meet (a NaN counts as both), a NaN.
+//
+// Class of element i of 16 bytes: bit 2 i: +inf or NaN, bit 2 i + 1: -inf or NaN.  (Whole
+// numbers throughout: conditions would be lane masks, which the kernels' loops have no
+// scalar registers for.)
+template <typename T>
+__device__ inline uint32_t not_finite(const uint4& x) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  uint32_t cls = 0;
+#pragma unroll
+  for (int i = 0; i < 16 / int(sizeof(T)); ++i) {
+    const uint32_t u = sizeof(T) == 4 ? w[i] : (i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+    const uint32_t m = u & 0x7fffffffu, nan = (m + 0x007fffffu) >> 31, minus = u >> 31;
+    const uint32_t odd = (m + 0x00800000u) >> 31;
+    cls |= (odd & (nan | (minus ^ 1u))) << (2 * i) | (odd & (nan | minus)) << (2 * i + 1);
+  }
+  return cls;
+}
+// Nonzero if 16 bytes hold any: an exponent of all ones carries into the sign's place.
+template <typename T>
+__device__ inline uint32_t any_not_finite(const uint4& x) {
+  constexpr uint32_t exps = sizeof(T) == 4 ? 0x7f800000u : 0x7f807f80u;
+  constexpr uint32_t one = sizeof(T) == 4 ? 0x00800000u : 0x00800080u;
+  return (((x.x & exps) + one) | ((x.y & exps) + one) | ((x.z & exps) + one) |
+          ((x.w & exps) + one)) & ~exps;
+}
+// the 16 bytes without the elements of `cls`
+template <typename T>
+__device__ inline uint4 finite_part(const uint4& x, uint32_t cls) {
+  uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+  for (int i = 0; i < 16 / int(sizeof(T)); ++i) {
+    const uint32_t keep = (((cls >> (2 * i) & 3u) + 3u) >> 2) - 1u;      // all ones, or zero
+    if constexpr (sizeof(T) == 4) w[i] &= keep;
+    else w[i / 2] &= i & 1 ? keep | 0x0000ffffu : keep | 0xffff0000u;
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// ones where `cls` has bit `sign` of an element
+template <typename T>
+__device__ inline uint4 ones_at(uint32_t cls, int sign) {
+  uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 16 / int(sizeof(T)); ++i) {
+    const uint32_t on = cls >> (2 * i + sign) & 1u;
+    if constexpr (sizeof(T) == 4) w[i] = on * 0x3f800000u;
+    else w[i / 2] |= on * (i & 1 ? 0x3f800000u : 0x3f80u);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// what a row's share of such elements adds
+__device__ inline float infinity_of(float share, int sign) {
+  return share > 0.f ? (sign ? -__builtin_huge_valf() : __builtin_huge_valf()) : 0.f;
+}
+
 // ----------------------------------------------------------------------------
-// few rows
+// single tokens
 // ----------------------------------------------------------------------------
 
-// A unit is 16 NB query rows; a workgroup's four wavefronts take contiguous quarters of
-// its tiles and meet only at a unit's end.  Scores are computed transposed, keys x rows,
+// A unit is up to 16 NB query rows of ONE token, so that all of them see the same keys and
+// nothing but the cache's end is masked; a workgroup's four wavefronts take contiguous
+// quarters of its tiles and meet only at a unit's end.  Scores are computed transposed, keys x rows,
 // in 16x16x32 MFMAs: lane l has column (query row) l % 16 and, of the 8 U keys that its
 // group j = l / 16 holds, all of a step's scores.  Keys are dealt to MFMA rows so that
 // these are 8 U consecutive keys, which is what the lane feeds to the P*V product, against
@@ -275,18 +333,18 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
 
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
   const int col = lane & 15, j = lane >> 4;
-  const int PS = a.pg.PS, limit = a.ch.max_pages * PS;
+  const int PS = a.pg.PS, limit = a.ch.max_pages * PS, rb = a.rb;
   stage_turns<D>(a, s_turns);
   // (fewer tiles a workgroup would leave wavefronts without a step)
   Place at;
-  const Share share = find_share<RB>(a, blockIdx.x, limit, I8 ? 4 : 2, at);
+  const Share share = find_share(a, blockIdx.x, rb, limit, I8 ? 4 : 2, at);
   Join join{};
   if (share.p0 == share.p1) {
     if (tid == 0) a.joins[blockIdx.x] = join;
     return;
   }
   unsigned p = share.p0;
-  Piece<RB> cur(a, limit, at, share.p1 - p);
+  Piece cur(a, rb, limit, at, share.p1 - p);
 
   // ---- loads of this wavefront's steps [s0, s1) of the current piece
   struct Set {
@@ -345,7 +403,7 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
     return I8 ? 64 * (c / 2) + 16 * j + 8 * (c % 2) : 32 * c + 8 * j;
   };
   uint32_t qx[NB][NQP][4], qy[NB][NQP][4];
-  int qpos[NB], qt[NB];                      // position, and token of the chunk
+  int qpos[NB];
   // a piece's queries and first steps
   auto enter = [&]() __attribute__((always_inline)) {
     const int n = (cur.t1 - cur.t0) * SPT;
@@ -355,10 +413,10 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       const unsigned row = cur.row0 + min(16 * nb + col, cur.nrows - 1);
-      qt[nb] = row / unsigned(a.G);
-      const T* qrow = static_cast<const T*>(a.q) + (cur.r.first + qt[nb]) * a.q_stride +
-                      size_t(cur.g * a.G + row - qt[nb] * a.G) * D;
-      qpos[nb] = a.rope.pos ? a.rope.pos[cur.r.first + qt[nb]] : 0;
+      const int t = row / unsigned(a.G);
+      const T* qrow = static_cast<const T*>(a.q) + (cur.r.first + t) * a.q_stride +
+                      size_t(cur.g * a.G + row - t * a.G) * D;
+      qpos[nb] = a.rope.pos ? a.rope.pos[cur.r.first + t] : 0;
 #pragma unroll
       for (int c = 0; c < NQP; ++c) {
         raw_load8<T>(qx[nb][c], qrow + qd(c) % (D / 2));
@@ -374,10 +432,8 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
   while (true) {
     // ---- queries: turned by their tokens' positions, the softmax scale folded in
     bf16x8 q[NB][NQC];
-    int sees[NB];                            // keys that this lane's rows see
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      sees[nb] = min(max(cur.r.base + qt[nb] + 1, 0), limit);
 #pragma unroll
       for (int c = 0; c < NQP; ++c) {
         float x[8], y[8];
@@ -393,8 +449,6 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
         }
       }
     }
-    const int sees_all = min(max(cur.r.base + int(unsigned(cur.row0) / unsigned(a.G)) + 1, 0),
-                             limit);         // every row's keys
     const int keys = cur.keys;
 
     float m_run[NB], m_ref[NB], l_run[NB];
@@ -409,7 +463,7 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
 
     auto compute = [&](int step, Set& x) __attribute__((always_inline)) {
       const int key0 = step * KS;
-      const bool partial = key0 + KS > sees_all || x.page < 0;
+      const bool partial = key0 + KS > keys || x.page < 0;
       bf16x8 pb[NB][U];
       f32x4 s[NB][2 * U];
 #pragma unroll
@@ -451,13 +505,12 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
             s[nb][k / 4][k % 4] = __builtin_fmaf(s[nb][k / 4][k % 4], ks[k], -m_ref[nb]);
       }
       if (partial) {
+        const int n = x.page < 0 ? 0 : keys - key0 - 8 * U * j;
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          const int n = x.page < 0 ? 0 : sees[nb] - key0 - 8 * U * j;
+        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
           for (int k = 0; k < 8 * U; ++k)
             if (k >= n) s[nb][k / 4][k % 4] = kNegInf;
-        }
         // what lies behind the last key may be anything
         if constexpr (I8) {
           if (key0 + lane >= keys) x.vs = 0.f;
@@ -531,12 +584,12 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
     }
 
     // ---- the next piece's first loads, under the end of this one
-    const Piece<RB> old = cur;
+    const Piece old = cur;
     p += old.t1 - old.t0;
     const bool more = p < share.p1;
     if (more) {
-      next_unit<RB>(a, limit, at);
-      cur = Piece<RB>(a, limit, at, share.p1 - p);
+      next_unit(a, rb, limit, at);
+      cur = Piece(a, rb, limit, at, share.p1 - p);
       enter();
     }
 
@@ -599,7 +652,7 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
 }
 
 // ----------------------------------------------------------------------------
-// many rows
+// blocks of rows
 // ----------------------------------------------------------------------------
 
 // Tiles of keys and transposed values in LDS, as 16-byte chunks of rows of D (keys) or 64
@@ -662,6 +715,7 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
   __shared__ __attribute__((aligned(1024)))
   uint8_t lds[NST * W::BYTES > XBYTES ? NST * W::BYTES : XBYTES];
   __shared__ double s_turns[D / 2];
+  __shared__ int s_odd[8];                       // a wavefront's values that are not finite
   const uint32_t lds0 = uint32_t(uintptr_t((__attribute__((address_space(3))) uint8_t*)lds));
 
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
@@ -674,7 +728,7 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
                                    : int(blockIdx.x);
   stage_turns<D>(a, s_turns);
   Place at;
-  const Share share = find_share<RB>(a, w, limit, 2, at);
+  const Share share = find_share(a, w, RB, limit, 2, at);
   Join join{};
   unsigned p = share.p0;
   lds_barrier();                                 // the turns are there
@@ -686,7 +740,7 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
   const uint32_t vofs = uint32_t(vrow * PS * SZ + vch * 16);
 
   while (p < share.p1) {
-    const Piece<RB> cur(a, limit, at, share.p1 - p);
+    const Piece cur(a, RB, limit, at, share.p1 - p);
     const int t0 = cur.t0, t1 = cur.t1, row0 = cur.row0, nrows = cur.nrows, keys = cur.keys;
     const int32_t* table = a.ch.table + size_t(at.b) * a.ch.max_pages;
     int ids = -1, ids_from = -(1 << 30);         // pages of tiles ids_from + lane
@@ -775,6 +829,9 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
     auto token_of = [&](int r) { return int(unsigned(row0 + min(r, nrows - 1)) / unsigned(a.G)); };
     const int sees_all = min(max(at.r.base + token_of(32 * rg) + 1, 0), limit);
     const int sees_any = min(max(at.r.base + token_of(32 * rg + 31) + 1, 0), limit);
+    const int sees_first = min(max(at.r.base + token_of(0) + 1, 0), limit);   // all rows' keys
+    // tiles [t0, end) have keys that rows of this wavefront see
+    const int end = rows_here ? (sees_any + ST - 1) / ST : t0;
     typename M::Op q[NQC * (F32 ? 4 : 1)];
     {
       const T* qrow = static_cast<const T*>(a.q) + (at.r.first + t) * a.q_stride +
@@ -872,8 +929,47 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
       }
       lds_barrier();
     };
+    // Takes values that are not finite out of a tile that some rows see and others do not;
+    // this thread's are `odd`, two bits an element.  True (for all wavefronts) if there are any.
+    uint32_t odd = 0;
+    static_assert(LV * W::EPC <= 16, "two bits for every element of a thread's chunks");
+    auto own_chunk = [&](int tile, int i) {
+      return reinterpret_cast<uint4*>(stage(tile) + W::KBYTES + (tid + i * NTH) * 16);
+    };
+    auto take_odd = [&](int tile) __attribute__((always_inline)) {
+      if ((tile + 1) * ST <= sees_first || sees_first >= keys) return false;
+      uint32_t quick = 0;
+#pragma unroll
+      for (int i = 0; i < LV; ++i) quick |= any_not_finite<T>(*own_chunk(tile, i));
+      const bool here = __any(quick);
+      if (lane == 0) s_odd[wave] = here;
+      lds_barrier();
+      int any = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) any |= s_odd[i];
+      if (!uniform(any)) return false;
+      odd = 0;
+#pragma unroll
+      for (int i = 0; i < LV; ++i) {
+        const uint32_t cls = not_finite<T>(*own_chunk(tile, i));
+        *own_chunk(tile, i) = finite_part<T>(*own_chunk(tile, i), cls);
+        odd |= cls << (2 * W::EPC * i);
+      }
+      lds_barrier();
+      return true;
+    };
+    // puts ones where they were
+    auto put_ones = [&](int tile, int sign) __attribute__((always_inline)) {
+      lds_barrier();
+#pragma unroll
+      for (int i = 0; i < LV; ++i)
+        *own_chunk(tile, i) = ones_at<T>(odd >> (2 * W::EPC * i), sign);
+      lds_barrier();
+    };
+
     // ---- one tile: scores, probabilities, P*V
-    auto compute = [&](int tile, int page, const uint8_t* st) __attribute__((always_inline)) {
+    auto compute = [&](int tile, int page, const uint8_t* st, bool strange)
+        __attribute__((always_inline)) {
       f32x16 s[NKB];
       if constexpr (F32) {
         static_assert(!F32 || NKB == 1, "an fp32 wavefront has one block of a tile");
@@ -939,6 +1035,27 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
           }
           o[db] += part;
         }
+        if (strange) {
+          for (int sign = 0; sign < 2; ++sign) {
+            put_ones(tile, sign);
+#pragma unroll
+            for (int db = 0; db < NDB; ++db) {
+              f32x16 part;
+#pragma unroll
+              for (int v = 0; v < 16; ++v) part[v] = 0.f;
+#pragma unroll
+              for (int c = 0; c < NPC; ++c) {
+                const float4 f = *reinterpret_cast<const float4*>(
+                    st + W::v_at(32 * db + col, 2 * (kg * NPC + c) + half));
+                const float fs[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) part = M::run(fs[e], s[0][4 * c + e], part);
+              }
+#pragma unroll
+              for (int v = 0; v < 16; ++v) o[db][v] += infinity_of(part[v], sign);
+            }
+          }
+        }
       } else {
         bf16x8 pb[NPC];
         const bf16x2 ones = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
@@ -971,12 +1088,38 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
           __builtin_amdgcn_sched_barrier(0);
         }
         __builtin_amdgcn_s_setprio(0);
+        if (strange) {
+          for (int sign = 0; sign < 2; ++sign) {
+            put_ones(tile, sign);
+#pragma unroll
+            for (int db = 0; db < NDB; ++db) {
+              f32x16 part;
+#pragma unroll
+              for (int v = 0; v < 16; ++v) part[v] = 0.f;
+#pragma unroll
+              for (int c = 0; c < NPC; ++c)
+                part = M::run(*reinterpret_cast<const bf16x8*>(
+                                  st + W::v_at(32 * db + col, 2 * (kg * NPC + c) + half)),
+                              pb[c], part);
+#pragma unroll
+              for (int v = 0; v < 16; ++v) o[db][v] += infinity_of(part[v], sign);
+            }
+          }
+        }
       }
       l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     };
+    // a tile that has arrived, by all wavefronts
+    auto work = [&](int tile, int page) __attribute__((always_inline)) {
+      const bool strange = take_odd(tile);
+      if (tile < end) {
+        compute(tile, page, stage(tile), strange);
+      } else if (strange) {
+        put_ones(tile, 0);
+        put_ones(tile, 1);
+      }
+    };
 
-    // tiles [t0, end) have keys that rows of this wavefront see
-    const int end = rows_here ? (sees_any + ST - 1) / ST : t0;
     if constexpr (I8) {
       commit_i8(t0);
       if (t0 + 1 < t1) load_i8(t0 + 1);
@@ -984,7 +1127,7 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
         lds_barrier();                           // this tile is there, the one before is read
         if (tile + 1 < t1) commit_i8(tile + 1);
         if (tile + 2 < t1) load_i8(tile + 2);
-        if (tile < end) compute(tile, page_id(tile), stage(tile));
+        work(tile, page_id(tile));
       }
     } else for (int tile = t0; tile < t1; ++tile) {
       // this tile's loads are done where only those of the tiles after it are in flight
@@ -996,7 +1139,7 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
       if (tile + NST - 1 < t1) load(tile + NST - 1);
       const int page = page_id(tile);
       clean(tile, page);
-      if (tile < end) compute(tile, page, stage(tile));
+      work(tile, page);
     }
 
     // ---- the key parts of a row group meet
@@ -1102,7 +1245,7 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
       }
     }
     p += t1 - t0;
-    if (p < share.p1) next_unit<RB>(a, limit, at);
+    if (p < share.p1) next_unit(a, RB, limit, at);
     lds_barrier();                               // LDS of this unit is read
   }
   if (tid == 0) a.joins[w] = join;
@@ -1217,14 +1360,24 @@ const void* join_fn(int rows) {
 
 }  // namespace
 
-AttendShape attend_shape(int store, int D, int64_t rows_max, int64_t batch, int64_t heads,
+AttendShape attend_shape(int store, int D, int64_t rows_max, int64_t max_chunk, int64_t batch,
+                         int64_t heads,
                          int64_t kv_max) {
   AttendShape s{};
   auto up = [](size_t x) { return (x + 255) & ~size_t(255); };
-  if (store == C2KV_F32) s.rows = 128;
-  else s.rows = rows_max <= 16 ? 16 : rows_max <= 32 ? 32 : rows_max <= 128 ? 128 : 256;
+  const int64_t G = rows_max / max_chunk;
+  // Single tokens: as many of a token's rows as divide them evenly, up to 32.  (Chunks of a
+  // few tokens run faster in blocks of rows, which read the keys once for all of them: 16
+  // requests of 3 to 7 drafts, 4 query heads a kv-head, 73 + 22 us in units of 32 mixed rows,
+  // 78 + 6 in blocks of 128.)  fp32 has the 128-row kernel only.
+  if (store != C2KV_F32 && max_chunk == 1) {
+    for (s.unit_rows = int(G < 32 ? G : 32); G % s.unit_rows != 0;) --s.unit_rows;
+    s.rows = s.unit_rows <= 16 ? 16 : 32;
+  } else {
+    s.rows = s.unit_rows = store == C2KV_F32 || rows_max <= 128 ? 128 : 256;
+  }
   const int64_t tiles =
-      batch * heads * ((rows_max + s.rows - 1) / s.rows) * ((kv_max + ST - 1) / ST);
+      batch * heads * ((rows_max + s.unit_rows - 1) / s.unit_rows) * ((kv_max + ST - 1) / ST);
   const int64_t most = s.rows <= 32 ? 512 : 256;   // two workgroups a CU, or one
   s.groups = int(tiles < most ? tiles : most);
   size_t at = 0;

@@ -71,6 +71,7 @@ struct AttendParams {
   PageView pg;
   RopeView rope;
   int32_t Hq, G;
+  int32_t rb;                   // query rows of a unit
   float qscale;                 // softmax scale * log2(e)
   const void* q;
   int64_t q_stride;
@@ -91,13 +92,15 @@ struct Join {
 
 // How an attention call is launched, and what its workspace holds.
 struct AttendShape {
-  int32_t rows;                 // RB: query rows of a unit
+  int32_t rows;                 // RB: query rows that a kernel's unit has room for
+  int32_t unit_rows;            // rows of a unit here, at most RB
   int32_t groups;               // workgroups
   size_t part_o, part_ml, joins, total;   // byte offsets
 };
-// rows_max: bound on the (token, query head) rows of one (request, kv-head), kv_max on a
-// request's cached tokens
-AttendShape attend_shape(int store, int D, int64_t rows_max, int64_t batch, int64_t heads,
+// rows_max: bound on the (token, query head) rows of one (request, kv-head), those of
+// max_chunk tokens; kv_max: bound on a request's cached tokens
+AttendShape attend_shape(int store, int D, int64_t rows_max, int64_t max_chunk, int64_t batch,
+                         int64_t heads,
                          int64_t kv_max);
 
 // `store`: type of the cache or pool; its activations are F32 for F32, else BF16.

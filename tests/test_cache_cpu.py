@@ -115,6 +115,24 @@ def test_refusals(kw, calls, status, text):
         assert st == status and text in msg, (name, st, msg)
 
 
+def test_attention_workspace_is_checked():
+    a, cfg, cache, ch = _args()
+    r, lib = ctypes.byref, c2kv.lib()
+    n = ctypes.c_size_t()
+    assert lib.c2kv_cache_attend_workspace(r(cfg), r(cache), r(ch), r(n)) == c2kv.C2KV_OK
+    assert n.value > 0
+    call = lambda ws, size: lib.c2kv_cache_attend(r(cfg), r(cache), r(ch), P, 0, None, P, None, ws,
+                                                  size, None)
+    for ws, size, text in ((None, n.value, "NULL"), (P + 128, n.value, "aligned"),
+                           (P, n.value - 1, "bytes")):
+        assert call(ws, size) == c2kv.C2KV_E_WORKSPACE
+        assert text in lib.c2kv_last_error().decode()
+    # more key tiles than the work line counts
+    a, cfg, cache, ch = _args(batch=1 << 20, n_tokens=1 << 20, max_pages=1 << 24, max_chunk=1)
+    for st in (lib.c2kv_cache_attend_workspace(r(cfg), r(cache), r(ch), r(n)), call(P, 1 << 40)):
+        assert st == UNSUP and "2^31" in lib.c2kv_last_error().decode()
+
+
 def test_null_descriptors_are_refused():
     a, cfg, cache, ch = _args()
     lib, r = c2kv.lib(), ctypes.byref

@@ -281,6 +281,65 @@ def test_attend_larger(shape, store):
     check_attend(s, out, lse, *dense64(s, s.q, s.pos.cpu().numpy()))
 
 
+@pytest.mark.parametrize("hints", [dict(max_chunk=1), dict(max_chunk=1, max_kv=1),
+                                   dict(max_chunk=2), dict(max_chunk=10_000, max_kv=1 << 30)])
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("i", [4, 5, 9])
+def test_bounds_that_do_not_hold_change_no_result(i, store, hints):
+    """max_chunk and max_kv choose launch shapes: chunks and caches beyond them are answered
+    as well (24 heads a kv-head of one token; ragged drafts; 130 tokens)."""
+    s = Scene(store, seed=60 + i, **ATTEND[i])
+    say(f"attend {store} {ATTEND[i]} {hints}")
+    out, lse = s.out(), s.lse()
+    c2kv.c2kv_cache_attend(s.cfg, s.cache, s.chunks(**hints), s.q, out, s.pos, lse)
+    torch.cuda.synchronize()
+    check_attend(s, out, lse, *dense64(s, s.q, s.pos.cpu().numpy()))
+
+
+@pytest.mark.parametrize("store", STORES)
+def test_prime_groups_and_many_requests(store):
+    """37 query heads a kv-head (no divisor up to 32), and 300 requests, some of them empty."""
+    for kw in (dict(n=[1, 1], ctx=[70, 500], hq=37, hkv=1, d=64),
+               dict(n=[(3 * i) % 4 for i in range(300)], ctx=[i % 90 for i in range(300)], hq=2,
+                    hkv=1, d=64)):
+        s = Scene(store, seed=31, **kw)
+        out, lse = s.out(), s.lse()
+        c2kv.c2kv_cache_attend(s.cfg, s.cache, s.chunks(max_chunk=max(s.n)), s.q, out, s.pos, lse)
+        torch.cuda.synchronize()
+        check_attend(s, out, lse, *dense64(s, s.q, s.pos.cpu().numpy()))
+
+
+def test_offsets_past_32_bits():
+    """A cache whose later pages lie beyond 2^32 elements from its start (4.4 GB each of keys
+    and values, int8): written, read back and attended there."""
+    hkv, d, page = 8, 128, 256
+    n_pages = (1 << 32) // (hkv * d * page) + 40
+    s = Scene("i8", [1, 90], [400, 130], hq=16, hkv=hkv, page=page, seed=33)
+    big = [torch.zeros((n_pages, hkv, *x), dtype=torch.int8, device="cuda")
+           for x in ((page, d), (d, page))]
+    scales = [torch.ones((n_pages, hkv, page), device="cuda") for _ in range(2)]
+    used = s.table >= 0
+    far = s.table.copy()
+    far[used] = n_pages - 1 - s.table[used]
+    for b in range(s.B):
+        for c in range(s.max_pages):
+            if s.table[b, c] >= 0:
+                for dst, src in zip((*big, *scales), (s.kp, s.vp, s.ks, s.vs)):
+                    dst[far[b, c]] = src[s.table[b, c]]
+    cache = c2kv.Cache(*big, *scales)
+    outs = []
+    for c, t in ((s.cache, s.table), (cache, far)):
+        ch = s.chunks(table=t)
+        c2kv.c2kv_cache_write(s.cfg, c, ch, s.k, s.v, s.pos)
+        k, v, o = torch.empty_like(s.k), torch.empty_like(s.v), s.out()
+        c2kv.c2kv_cache_read(s.cfg, c, ch, k, v)
+        c2kv.c2kv_cache_attend(s.cfg, c, ch, s.q, o, s.pos)
+        outs.append((k, v, o))
+    torch.cuda.synchronize()
+    for a, b in zip(*outs):
+        assert torch.equal(a, b)
+
+
 @pytest.mark.parametrize("store", STORES)
 @pytest.mark.parametrize("shape", [dict(n=[1, 1, 1, 1, 1], ctx=[10, 200, 300, 64, 30]),
                                    dict(n=[5, 90, 2, 40, 3], ctx=[10, 200, 300, 64, 30])])
@@ -369,6 +428,45 @@ def test_attend_nan_query_stays_in_its_row():
     assert torch.isnan(out2[1, 3]).all() and torch.isnan(out2[20, 0]).all()
     out2[1, 3], out2[20, 0] = out[1, 3], out[20, 0]
     assert torch.isfinite(out2).all()
+
+
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("n,hq", [([5, 3], 8), ([40, 90], 8), ([300, 70], 2), ([9, 2], 24)])
+def test_attend_values_that_later_tokens_see(n, hq, store):
+    """Infinities and NaN in the values (and keys) of a chunk's own tokens reach the tokens
+    that see them, column by column, and no token before them."""
+    s = Scene(store, n, [70, 130], hq=hq, hkv=2, seed=21)
+    say(f"values not finite {store} {n}")
+    out = s.out()
+    c2kv.c2kv_cache_attend(s.cfg, s.cache, s.chunks(), s.q, out, s.pos)
+    where = cache_oracle.places(s.tok_off, s.kv_len, s.table, s.page, s.n_pages, s.n_tokens)
+    inf, nan = float("inf"), float("nan")
+    want = out.clone().float()
+    G = hq // s.hkv
+    for b, (t, h, d, x) in enumerate([(n[0] // 2, 0, 7, inf), (n[1] - 1, 1, 100, nan)]):
+        r0, r1 = int(s.tok_off[b]), int(s.tok_off[b + 1])
+        _, _, page, at = where[r0 + t]
+        heads = slice(h * G, (h + 1) * G)
+        if store == "i8":
+            s.vs[page, h, at] = nan
+            want[r0 + t:r1, heads] = nan
+        else:
+            s.vp[page, h, d, at] = x
+            want[r0 + t:r1, heads, d] = x
+            if b == 0:                       # and one of each sign in another column
+                s.vp[page, h, d + 1, at] = -inf
+                want[r0 + t:r1, heads, d + 1] = -inf
+                s.vp[where[r0 + t + 1][2], h, d + 1, where[r0 + t + 1][3]] = inf
+                want[r0 + t + 1:r1, heads, d + 1] = nan
+    out2 = s.out()
+    c2kv.c2kv_cache_attend(s.cfg, s.cache, s.chunks(), s.q, out2, s.pos)
+    torch.cuda.synchronize()
+    got = out2.float()
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    assert torch.equal(torch.isinf(got), torch.isinf(want))
+    fine = torch.isfinite(want)
+    assert torch.equal(got[fine], want[fine])
+    assert torch.equal(got[torch.isinf(want)], want[torch.isinf(want)])
 
 
 def test_attend_large_scores():

@@ -220,6 +220,8 @@ def dense64(s, q, pos, lens=None):
     for b in range(s.B):
         r0, r1, n = int(s.tok_off[b]), int(s.tok_off[b + 1]), int(s.kv_len[b])
         has[r0:r1] = True
+        if n == 0:
+            continue
         ids = s.table[b][:-(-n // s.page)]
         k = torch.from_numpy(np.concatenate([kp[i] for i in ids], 1)[:, :n]).cuda()
         v = torch.from_numpy(np.concatenate([vp[i] for i in ids], 2)[:, :, :n]).cuda()

@@ -220,6 +220,13 @@ __device__ inline bf16x8 bf16_of(const float (&x)[8]) {
                              pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
   return __builtin_bit_cast(bf16x8, u);
 }
+// what bf16_of left of x
+__device__ inline bf16x8 rest_of(const float (&x)[8], const bf16x8& hi) {
+  float r[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r[e] = x[e] - static_cast<float>(hi[e]);
+  return bf16_of(r);
+}
 __device__ inline bf16x8 bf16_of_i8(uint32_t w0, uint32_t w1) {
   const uint32_t w[2] = {w0, w1};
   float x[8];
@@ -313,7 +320,11 @@ __device__ inline float infinity_of(float share, int sign) {
 // in flight (one where 32 rows leave no registers for the second).
 //
 // int8 codes become bf16 exactly; key scales multiply the scores, value scales the
-// probabilities, in fp32.
+// probabilities, in fp32.  A turned query is held as two bf16 numbers, the second what the
+// first leaves: rounded to one, it would be the largest error of the output (queries of
+// standard deviation 2: 2-norm 0.0041 of the output's, 0.0024 with both, of which 0.0017 are
+// the output's own rounding).  Both come from LDS every step, and the MFMAs that the second
+// adds are idle time here.
 template <typename S, int D, int NB>
 __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
   using T = __bf16;
@@ -330,6 +341,7 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
   __shared__ __attribute__((aligned(16))) float s_o[NW * RB * LDO];
   __shared__ float s_m[NW * RB], s_l[NW * RB];
   __shared__ double s_turns[D / 2];
+  __shared__ bf16x8 s_q[NB * NQC * 64], s_rest[NB * NQC * 64];   // (every wavefront's the same)
 
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
   const int col = lane & 15, j = lane >> 4;
@@ -431,7 +443,6 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
 
   while (true) {
     // ---- queries: turned by their tokens' positions, the softmax scale folded in
-    bf16x8 q[NB][NQC];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
@@ -440,12 +451,19 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
         raw_to_f8<T>(qx[nb][c], x);
         raw_to_f8<T>(qy[nb][c], y);
         turn_chunks<8>(s_turns + qd(c) % (D / 2), a.rope.pos, qpos[nb], a.qscale, x, y);
+        auto put = [&](int i, const float (&v)[8]) __attribute__((always_inline)) {
+          const bf16x8 hi = bf16_of(v);
+          s_q[(nb * NQC + i) * 64 + lane] = hi;
+          s_rest[(nb * NQC + i) * 64 + lane] = rest_of(v, hi);
+        };
         if constexpr (NQP < NQC) {
-          q[nb][c] = bf16_of(x);
-          q[nb][c + NQP] = bf16_of(y);
+          put(c, x);
+          put(c + NQP, y);
         } else {
-          const bf16x8 lo = bf16_of(x), hi = bf16_of(y);
-          q[nb][c] = qd(c) < D / 2 ? lo : hi;
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = qd(c) < D / 2 ? x[e] : y[e];
+          put(c, v);
         }
       }
     }
@@ -467,7 +485,7 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
       bf16x8 pb[NB][U];
       f32x4 s[NB][2 * U];
 #pragma unroll
-      for (int m = 0; m < 2 * U; ++m) {
+      for (int m = 0; m < 2 * U; ++m)
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
           // bf16: scores leave the product relative to the reference
@@ -475,24 +493,29 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
           s[nb][m] = f32x4{z, z, z, z};
         }
 #pragma unroll
-        for (int c = 0; c < NKC; ++c) {
-          const u32x4 w = x.k[m * NKC + c];
+      for (int c = 0; c < NQC; ++c) {
+        bf16x8 q[NB], rest[NB];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          q[nb] = s_q[(nb * NQC + c) * 64 + lane];
+          rest[nb] = s_rest[(nb * NQC + c) * 64 + lane];
+        }
+#pragma unroll
+        for (int m = 0; m < 2 * U; ++m) {
+          bf16x8 kf;
           if constexpr (I8) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const bf16x8 kf = bf16_of_i8(w[2 * h], w[2 * h + 1]);
-#pragma unroll
-              for (int nb = 0; nb < NB; ++nb)
-                s[nb][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[nb][2 * c + h], s[nb][m],
-                                                                   0, 0, 0);
-            }
+            const u32x4 w = x.k[m * NKC + c / 2];
+            kf = bf16_of_i8(w[2 * (c % 2)], w[2 * (c % 2) + 1]);
           } else {
-            const bf16x8 kf = __builtin_bit_cast(bf16x8, w);
+            kf = __builtin_bit_cast(bf16x8, x.k[m * NKC + c]);
+          }
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
-              s[nb][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[nb][c], s[nb][m], 0, 0, 0);
+          for (int nb = 0; nb < NB; ++nb) {
+            s[nb][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[nb], s[nb][m], 0, 0, 0);
+            s[nb][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, rest[nb], s[nb][m], 0, 0, 0);
           }
         }
+        __builtin_amdgcn_sched_barrier(0);     // (one chunk's queries at a time)
       }
       if constexpr (I8) {
         // lane l has the scale of key key0 + l, and scores of its group's 16 keys
@@ -686,9 +709,11 @@ __device__ inline void wait_loads_barrier() {
 // 8 consecutive keys at a time (keys are dealt to the MFMA's rows with bits 2 and 3 of
 // their index exchanged), the operand of the P*V product.
 //
-// int8 tiles go through registers, decoded (code * scale in fp32) and rounded to bf16 once,
-// as c2kv_compose decodes them: applied to scores and probabilities instead, the scales
-// would cost every wavefront what here costs the workgroup once.
+// int8 codes go through registers.  Keys become bf16 exactly and their scales multiply the
+// scores in fp32; values are decoded there (code * scale in fp32) and rounded once, as
+// c2kv_compose rounds them.  (2048 tokens over 32k, 32 query heads: 1.30 ms.  Keys decoded and
+// rounded too: 1.14, but the 2-norm of the error is then 0.0052 of the output's, not 0.0045;
+// value scales applied to the probabilities instead: 1.35, and 0.0042.)
 template <typename T, typename S, int D, int RG>
 __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
   using M = Mma<T>;
@@ -698,7 +723,12 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
   constexpr int KG = 8 / RG, NKB = 2 / KG;       // key parts, 32-key blocks of a wavefront
   static_assert(KG <= 2, "a wavefront has a 32-key block at least");
   constexpr int RB = 32 * RG;
-  constexpr int NST = F32 || I8 ? 2 : 4;         // tiles in LDS
+  // Queries held as two bf16 numbers, as for single tokens, where 128 rows a workgroup leave
+  // the MFMAs idle (16 requests of 3 to 7 drafts: 81 -> 84 us).  256 rows would pay half as
+  // many products again for the scores (2048 tokens over 32k: 1.06 -> 1.43 ms): there a turned
+  // and scaled query is rounded once, as c2kv_attend's are.
+  constexpr bool TWO = !F32 && RG == 4;
+  constexpr int NST = F32 || I8 ? 2 : TWO ? 3 : 4;   // tiles in LDS
   constexpr int LK = ST * W::CK / NTH, LV = D * W::CV / NTH, LPT = LK + LV;
   constexpr int NQC = W::CK / 2;                 // query chunks of a lane (its half's)
   constexpr int NPC = 16 * NKB / W::EPC;         // probability chunks of a lane
@@ -716,6 +746,8 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
   uint8_t lds[NST * W::BYTES > XBYTES ? NST * W::BYTES : XBYTES];
   __shared__ double s_turns[D / 2];
   __shared__ int s_odd[8];                       // a wavefront's values that are not finite
+  __shared__ bf16x8 s_rest[TWO ? RG * NQC * 64 : 1];
+  __shared__ float s_scale[I8 ? NST * ST : 1];   // int8: of a tile's keys
   const uint32_t lds0 = uint32_t(uintptr_t((__attribute__((address_space(3))) uint8_t*)lds));
 
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
@@ -771,8 +803,8 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
     // keys of a tile that exist
     auto there = [&](int tile, int page) { return page < 0 ? 0 : min(max(keys - tile * ST, 0), ST); };
 
-    // int8: BPT codes of a key (elements ikd ..) and of a value row (keys ivk ..) a thread.
-    // Lane l has the value scale of key l, and a value row's keys of its own group of 16.
+    // int8: BPT codes of a key (elements ikd ..) and of a value row (keys ivk ..) a thread;
+    // lane l has the scales of key l
     constexpr int BPT = ST * D / NTH;
     const int ikey = tid / (D / BPT), ikd = tid % (D / BPT) * BPT;
     const int ivd = wave * BPT + lane % BPT, ivk = lane / BPT * BPT;
@@ -789,25 +821,24 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
         raw_load8<int8_t>(vraw + 2 * i, vp + 8 * i);
       }
       vscale = a.pg.v_scale[ph * PS + off + lane];
-      kscale = a.pg.k_scale[ph * PS + off + ikey];
+      kscale = a.pg.k_scale[ph * PS + off + lane];
     };
     auto commit_i8 = [&](int tile) __attribute__((always_inline)) {
       const int n = there(tile, page_id(tile));
       // (a scale behind the last key may be anything)
       float vs[16];
       lanes16(lane < n ? vscale : 0.f, vs, std::make_integer_sequence<int, 16>{});
+      if (wave == 0) s_scale[unsigned(tile - t0) % NST * ST + lane] = kscale;
       uint8_t* st = stage(tile);
 #pragma unroll
       for (int i = 0; i < BPT / 8; ++i) {
-        float x[8], y[8];
-        raw_to_f8<int8_t>(kraw + 2 * i, x);
+        *reinterpret_cast<bf16x8*>(st + W::k_at(ikey, ikd / 8 + i)) =
+            bf16_of_i8(kraw[2 * i], kraw[2 * i + 1]);
+        float y[8];
         raw_to_f8<int8_t>(vraw + 2 * i, y);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          x[e] *= kscale;
+        for (int e = 0; e < 8; ++e)
           y[e] *= BPT == 16 ? vs[8 * i + e] : lane & 8 ? vs[8 + e] : vs[e];
-        }
-        *reinterpret_cast<bf16x8*>(st + W::k_at(ikey, ikd / 8 + i)) = bf16_of(x);
         *reinterpret_cast<bf16x8*>(st + W::v_at(ivd, ivk / 8 + i)) = bf16_of(y);
       }
     };
@@ -871,6 +902,10 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
         } else {
           q[c] = bf16_of(x);
           q[c + NQC / 2] = bf16_of(y);
+          if constexpr (TWO) {                   // (the same from both key parts)
+            s_rest[(rg * NQC + c) * 64 + lane] = rest_of(x, q[c]);
+            s_rest[(rg * NQC + c + NQC / 2) * 64 + lane] = rest_of(y, q[c + NQC / 2]);
+          }
         }
       }
     }
@@ -912,8 +947,10 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
         for (int b = 0; b < NKB; ++b)
 #pragma unroll
           for (int v = 0; v < 16; ++v) s[b][v] -= d;
+        if constexpr (!I8) {
 #pragma unroll
-        for (int v = 0; v < 16; ++v) bias[v] = -ref;
+          for (int v = 0; v < 16; ++v) bias[v] = -ref;
+        }
         m_run = m_new;
         m_ref = ref;
       }
@@ -991,19 +1028,38 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
           return *reinterpret_cast<const bf16x8*>(
               st + W::k_at(kr + 32 * (f / NQC), 2 * (f % NQC) + half));
         };
-        bf16x8 kf[AH];
+        bf16x8 kf[AH], rf[AH];
 #pragma unroll
-        for (int f = 0; f < AH; ++f) kf[f] = frag(f);
+        for (int f = 0; f < AH; ++f) {
+          kf[f] = frag(f);
+          if constexpr (TWO) rf[f] = s_rest[(rg * NQC + f % NQC) * 64 + lane];
+        }
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);           // matrix work before the other's softmax
 #pragma unroll
         for (int f = 0; f < NF; ++f) {
           const int b = f / NQC, c = f % NQC;
           s[b] = M::run(kf[f % AH], q[c], c == 0 ? bias : s[b]);
+          if constexpr (TWO) {
+            s[b] = M::run(kf[f % AH], rf[f % AH], s[b]);
+            if (f + AH < NF) rf[f % AH] = s_rest[(rg * NQC + (f + AH) % NQC) * 64 + lane];
+          }
           if (f + AH < NF) kf[f % AH] = frag(f + AH);
           __builtin_amdgcn_sched_barrier(0);
         }
         __builtin_amdgcn_s_setprio(0);
+      }
+      if constexpr (I8) {
+#pragma unroll
+        for (int b = 0; b < NKB; ++b) {
+          // of this lane's 16 scores, from its group of 16 lanes
+          float ks[16];
+          lanes16(s_scale[unsigned(tile - t0) % NST * ST + 32 * (kg * NKB + b) +
+                          16 * (lane >> 3 & 1) + 8 * half + (lane & 7)],
+                  ks, std::make_integer_sequence<int, 16>{});
+#pragma unroll
+          for (int v = 0; v < 16; ++v) s[b][v] = __builtin_fmaf(s[b][v], ks[v], -m_ref);
+        }
       }
 #pragma unroll
       for (int b = 0; b < NKB; ++b) mask(tile, b, page, s[b]);
@@ -1060,17 +1116,17 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
         bf16x8 pb[NPC];
         const bf16x2 ones = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
 #pragma unroll
-        for (int c = 0; c < NPC; ++c)
+        for (int b = 0; b < NKB; ++b) {
 #pragma unroll
-          for (int e = 0; e < 8; e += 2) {
-            const f32x2 x = {__builtin_amdgcn_exp2f(s[c / 2][8 * (c % 2) + e]),
-                             __builtin_amdgcn_exp2f(s[c / 2][8 * (c % 2) + e + 1])};
-            const bf16x2 b = __builtin_convertvector(x, bf16x2);
-            pb[c][e] = b[0];
-            pb[c][e + 1] = b[1];
+          for (int v = 0; v < 16; v += 2) {
+            const f32x2 x = {__builtin_amdgcn_exp2f(s[b][v]), __builtin_amdgcn_exp2f(s[b][v + 1])};
+            const bf16x2 w = __builtin_convertvector(x, bf16x2);
+            pb[2 * b + v / 8][v % 8] = w[0];
+            pb[2 * b + v / 8][v % 8 + 1] = w[1];
             // the sum of the rounded values that the product uses
-            sum[e / 2] = __builtin_amdgcn_fdot2_f32_bf16(b, ones, sum[e / 2], false);
+            sum[v / 2 % 4] = __builtin_amdgcn_fdot2_f32_bf16(w, ones, sum[v / 2 % 4], false);
           }
+        }
         constexpr int NF = NPC * NDB, AH = 4;
         auto frag = [&](int f) __attribute__((always_inline)) {
           return *reinterpret_cast<const bf16x8*>(

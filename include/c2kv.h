@@ -343,8 +343,8 @@ typedef struct c2kv_chunks {
   const int32_t* block_table;  /* [B][max_pages] DEVICE                            */
   int32_t max_pages;           /* columns of the block table, >= 1                 */
   int32_t max_chunk;           /* a bound on n_b and one on kv_len, for launch     */
-  int32_t max_kv;              /* shapes only (any value gives the same results;
-                                  0: n_tokens and max_pages * page_size)           */
+  int32_t max_kv;              /* shapes only (every token is answered whatever they
+                                  say; 0: n_tokens and max_pages * page_size)      */
 } c2kv_chunks;
 
 /* Write each chunk's tokens into the cache.  k, v [n_tokens][H_kv][D] in the act dtype,
@@ -374,7 +374,8 @@ c2kv_status c2kv_cache_read(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,
  * natural-log (NULL to skip).  A token that sees no key gets zeros and an lse of -inf;
  * what lies in pages behind the last cached token has no effect, whatever it is.
  * workspace: device memory on 256 bytes, of c2kv_cache_attend_workspace's size; calls
- * that share one must be ordered.  It need not be cleared. */
+ * that share one must be ordered.  It need not be cleared.  out must not overlap q, nor
+ * in any of these calls what is written what is read. */
 c2kv_status c2kv_cache_attend_workspace(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,
                                         const c2kv_chunks* chunks, size_t* bytes);
 c2kv_status c2kv_cache_attend(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,

@@ -428,7 +428,12 @@ def _run(fn, dev: int, stream, *args):
     if t._C._cuda_getDevice() != dev:
         with t.cuda.device(dev):
             return _run(fn, dev, stream, *args)
-    s = t._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    if stream is None:
+        s = t._C._cuda_getCurrentRawStream(dev)
+    elif stream.device_index != dev:
+        raise ValueError(f"a stream of device {stream.device_index}, tensors on {dev}")
+    else:
+        s = stream.cuda_stream
     status = fn(*args, s)
     if status != C2KV_OK:
         _check(status)
@@ -449,6 +454,8 @@ def _rows(t, cfg: AttnCfg, heads: int, n: int, dev: int, what: str):
     s0, s1, s2 = t.stride()
     if s2 != 1 or (s1 != d and heads > 1):
         raise ValueError(f"the heads of {what} must be dense")
+    if shape[0] > 1 and s0 < heads * d:        # (the library takes a stride of 0 as dense)
+        raise ValueError(f"the tokens of {what} overlap (stride {s0})")
     return t.data_ptr(), s0 if shape[0] > 1 else 0
 
 

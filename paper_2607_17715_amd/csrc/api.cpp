@@ -190,8 +190,13 @@ c2kv_status check_cache(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,
     return fail(C2KV_E_INVAL, "tok_off, kv_len and block_table must not be NULL");
   if (int64_t(ch->max_pages) * cache->page_size > (1ll << 30))
     return fail(C2KV_E_UNSUPPORTED, "block tables of more than 2^30 tokens are not built");
-  if (int64_t(ch->n_tokens) * cfg->n_q_heads > (1ll << 31) - 1 || ch->batch > (1 << 28))
+  if (int64_t(ch->n_tokens) * cfg->n_q_heads > (1ll << 31) - 1)
     return fail(C2KV_E_UNSUPPORTED, "chunks of 2^31 (token, head) rows or more are not built");
+  // (a launch counts its threads in 32 bits: 256 for each tile of tokens)
+  if (ch->n_tokens > 1 << 29)
+    return fail(C2KV_E_UNSUPPORTED, "chunks of more than 2^29 tokens are not built");
+  if (ch->batch > 1 << 22)
+    return fail(C2KV_E_UNSUPPORTED, "batches of more than 2^22 requests are not built");
   return C2KV_OK;
 }
 
@@ -637,6 +642,7 @@ c2kv_status c2kv_pool_write(const c2kv_attn_cfg* cfg, const c2kv_pool* pool, int
     if (st != C2KV_OK) return st;
     if (n < 0 || pool->n_rows < 0) return fail(C2KV_E_INVAL, "n and n_rows must be >= 0");
     if (n == 0) return C2KV_OK;
+    if (n > 1 << 28) return fail(C2KV_E_UNSUPPORTED, "more than 2^28 rows a call are not built");
     if (!row) return fail(C2KV_E_INVAL, "row must not be NULL");
     st = check_rows("k", *cfg, k, cfg->n_kv_heads, k_stride);
     if (st == C2KV_OK) st = check_rows("v", *cfg, v, cfg->n_kv_heads, v_stride);

@@ -1417,8 +1417,7 @@ const void* join_fn(int rows) {
 }  // namespace
 
 AttendShape attend_shape(int store, int D, int64_t rows_max, int64_t max_chunk, int64_t batch,
-                         int64_t heads,
-                         int64_t kv_max) {
+                         int64_t heads, int64_t kv_max) {
   AttendShape s{};
   auto up = [](size_t x) { return (x + 255) & ~size_t(255); };
   const int64_t G = rows_max / max_chunk;
@@ -1432,8 +1431,9 @@ AttendShape attend_shape(int store, int D, int64_t rows_max, int64_t max_chunk, 
   } else {
     s.rows = s.unit_rows = store == C2KV_F32 || rows_max <= 128 ? 128 : 256;
   }
-  const int64_t tiles =
-      batch * heads * ((rows_max + s.unit_rows - 1) / s.unit_rows) * ((kv_max + ST - 1) / ST);
+  const double tiles = double(batch) * double(heads) *
+                       double((rows_max + s.unit_rows - 1) / s.unit_rows) *
+                       double((kv_max + ST - 1) / ST);   // (may pass 64 bits)
   const int64_t most = s.rows <= 32 ? 512 : 256;   // two workgroups a CU, or one
   s.groups = int(tiles < most ? tiles : most);
   size_t at = 0;

@@ -100,8 +100,7 @@ struct AttendShape {
 // rows_max: bound on the (token, query head) rows of one (request, kv-head), those of
 // max_chunk tokens; kv_max: bound on a request's cached tokens
 AttendShape attend_shape(int store, int D, int64_t rows_max, int64_t max_chunk, int64_t batch,
-                         int64_t heads,
-                         int64_t kv_max);
+                         int64_t heads, int64_t kv_max);
 
 // `store`: type of the cache or pool; its activations are F32 for F32, else BF16.
 hipError_t launch_cache_write(const WriteParams& p, int store, int D, int max_chunk,

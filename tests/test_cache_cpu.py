@@ -133,6 +133,24 @@ def test_attention_workspace_is_checked():
         assert st == UNSUP and "2^31" in lib.c2kv_last_error().decode()
 
 
+@pytest.mark.parametrize("kw,calls,text", [
+    (dict(hq=1, hkv=1, n_tokens=(1 << 29) + 1), CACHE, "2^29 tokens"),
+    (dict(batch=(1 << 22) + 1), CACHE, "2^22 requests"),
+    (dict(n_tokens=(1 << 28) + 1, hq=1, hkv=1), ("pool",), "2^28 rows"),
+    # products of bounds that pass 64 bits
+    (dict(hq=65535, hkv=65535, batch=1 << 22, n_tokens=1 << 15, max_pages=1 << 24),
+     ("attend", "workspace"), "2^31 key tiles"),
+    (dict(hq=1, hkv=1, batch=1 << 22, n_tokens=1 << 29, max_pages=1 << 24),
+     ("attend", "workspace"), "2^31 key tiles"),
+])
+def test_what_a_launch_cannot_count_is_refused(kw, calls, text):
+    built = _args(**kw)
+    for name in calls:
+        st = _calls(*built)[name]()
+        msg = c2kv.lib().c2kv_last_error().decode()
+        assert st == UNSUP and text in msg, (name, st, msg)
+
+
 def test_null_descriptors_are_refused():
     a, cfg, cache, ch = _args()
     lib, r = c2kv.lib(), ctypes.byref
@@ -168,6 +186,27 @@ def test_binding_refuses_shapes_and_types():
         c2kv.Chunks(i(3), i(2).long(), i(2, 4), 5)
     with pytest.raises(ValueError):                      # one offset missing
         c2kv.Chunks(i(2), i(2), i(2, 4), 5)
+
+
+def test_binding_refuses_rows_that_overlap():
+    """A token stride of 0 (an expanded row) means dense rows to the library."""
+    cfg = c2kv.attn_cfg(2, 2, 64, "bf16", 1e4)
+    rows = lambda t: c2kv._rows(t, cfg, 2, 3, t.get_device(), "k")
+    base = torch.zeros(8, 2, 64, dtype=torch.bfloat16)
+    c2kv._torch()
+    assert rows(base) == (base.data_ptr(), 128)
+    assert rows(base[::2]) == (base.data_ptr(), 256)
+    for t in (base[:1].expand(4, 2, 64), base.flatten().as_strided((4, 2, 64), (64, 64, 1))):
+        with pytest.raises(ValueError, match="overlap"):
+            rows(t)
+
+
+def test_binding_refuses_a_stream_of_another_device(monkeypatch):
+    class Stream:
+        device_index, cuda_stream = 1, 0
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    with pytest.raises(ValueError, match="stream of device 1"):
+        c2kv._run(lambda *a: pytest.fail("launched"), 0, Stream())
 
 
 def test_cache_oracle_equals_composed_attention():

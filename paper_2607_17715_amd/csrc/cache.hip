@@ -165,8 +165,9 @@ struct ValueTile {
 // write
 // ----------------------------------------------------------------------------
 
-// A wavefront per (token, kv-head): lane i holds the key pair (i, i + D/2).  For steps of
-// few tokens a request: bound by latency (two dependent loads: the requests, the page).
+// A wavefront per (token, kv-head): lane i holds the key pair (i, i + D/2).  For few tokens,
+// or few of each request: bound by latency (two dependent loads: the requests, the page; 24
+// requests' tokens, 8 heads of 128 in bf16: 4.0 us, an empty launch's time).
 template <typename T, typename S, int D>
 __global__ __launch_bounds__(256) void write_rows_kernel(WriteParams a) {
   constexpr int VPL = D / 64;                // values per lane
@@ -534,8 +535,13 @@ hipError_t launch_cache_write(const WriteParams& p, int store, int D, int max_ch
     using T = decltype(t);
     using S = decltype(s);
     constexpr int kD = decltype(d)::value;
-    if (max_chunk <= 8) {
-      const int64_t units = int64_t(p.ch.n_tokens) * p.pg.Hkv;
+    // A wavefront a (token, kv-head) ends soonest where all of them run at once, or where a
+    // tile would hold few tokens; else tiles, which write whole lines (bf16, 8 heads of 128,
+    // rows against tiles: 256 tokens 5.4 | 6.1 us, 512 6.8 | 6.3; 128 requests of 1 token
+    // 5.6 | 11.4, of 8 12.1 | 12.2, of 32 26.9 | 18.2).  (A launch counts its threads, 64 a
+    // unit, in 32 bits.)
+    const int64_t units = int64_t(p.ch.n_tokens) * p.pg.Hkv;
+    if (units <= 2048 || (max_chunk <= 8 && units < 1 << 26)) {
       return launch(reinterpret_cast<const void*>(&write_rows_kernel<T, S, kD>),
                     dim3(unsigned((units + 3) / 4)), dim3(256), st, p, e0, e1);
     }

@@ -49,6 +49,10 @@ SHAPES = [
     dict(n=[64, 64], ctx=[0, 64], d=64, hq=4, hkv=4, page=128),
     dict(n=[257], ctx=[61], hq=2, hkv=1, page=192, d=64, far=1_000_000),
     dict(n=[2] * 70 + [9], ctx=list(range(71)), hq=2, hkv=1, d=64),
+    # more (token, head) pairs than run at once: tiles for longer chunks, rows for hinted ones
+    dict(n=[300, 1, 0, 77, 64, 129], ctx=[10, 64, 3, 127, 5, 62], hkv=8, fused=True, pad_rows=3),
+    dict(n=[700, 33], ctx=[61, 100], hkv=4, d=64, page=192, far=1_000_000),
+    dict(n=[64] * 33 + [5], ctx=list(range(34)), hq=3, hkv=1),
 ]
 
 
@@ -146,6 +150,24 @@ def test_int8_rows_of_zeros_infinities_and_nans():
             assert not torch.isfinite(t[i, h]).any()
             assert torch.isfinite(t[i, 1 - h]).all()
         assert torch.isfinite(rk[5:]).all() and torch.isfinite(rv[4:]).all()
+
+
+def test_int8_tiles_of_zeros_infinities_and_nans():
+    s = Scene("i8", [1200], [7], seed=4)
+    s.k[3] = 0
+    s.k[500, 1, 5] = float("inf")
+    s.v[501, 0, 9] = float("nan")
+    s.v[502, 0] = 2.0 ** -110
+    c2kv.c2kv_cache_write(s.cfg, s.cache, s.chunks(), s.k, s.v)
+    torch.cuda.synchronize()
+    where = cache_oracle.places(s.tok_off, s.kv_len, s.table, s.page, s.n_pages, s.n_tokens)
+    kp, vp = s.pages64()
+    key = lambda i, h: kp[where[i][2], h, where[i][3]]
+    value = lambda i, h: vp[where[i][2], h, :, where[i][3]]
+    assert (key(3, 0) == 0).all() and (key(3, 1) == 0).all()
+    assert np.isnan(key(500, 1)).all() and np.isfinite(key(500, 0)).all()
+    assert np.isnan(value(501, 0)).all() and np.isfinite(value(501, 1)).all()
+    assert (value(502, 0) == 0).all() and (value(502, 1) != 0).any()
 
 
 @pytest.mark.parametrize("store", STORES)
@@ -364,6 +386,28 @@ def test_attend_missing_pages_and_lengths(shape, store):
     ref = cache_oracle.attend(f64(s.q), s.pos.cpu().numpy(), kp, vp, s.tok_off, s.kv_len,
                               s.table, s.base)
     check_attend(s, out, lse, *ref)
+
+
+@pytest.mark.parametrize("store", STORES)
+def test_write_skips_missing_pages_of_long_chunks(store):
+    s = Scene(store, [700, 3, 500], [10, 0, 5], seed=9)
+    s.table[0, 1] = -1
+    s.table[2, 0] = s.n_pages
+    s.kv_len[1] = 1
+    where = cache_oracle.places(s.tok_off, s.kv_len, s.table, s.page, s.n_pages, s.n_tokens)
+    rows = np.array([r for r in sorted(where) if where[r][2] is not None])
+    for t in (s.kp, s.vp):
+        t.zero_()
+    c2kv.c2kv_cache_write(s.cfg, s.cache, s.chunks(), s.k, s.v)
+    torch.cuda.synchronize()
+    assert (f64(s.kp) != 0).any((1, 3)).sum() == len(rows)
+    assert (f64(s.vp) != 0).any((1, 2)).sum() == len(rows)
+    page = np.array([where[r][2] for r in rows])
+    at = np.array([where[r][3] for r in rows])
+    kp, vp = s.pages64()
+    tol = dict(f32=0, bf16=0, i8=0.03)[store]
+    assert np.abs(kp[page, :, at] - f64(s.k)[rows]).max() <= tol
+    assert np.abs(vp[page, :, :, at] - f64(s.v)[rows]).max() <= tol
 
 
 @pytest.mark.parametrize("store", STORES)

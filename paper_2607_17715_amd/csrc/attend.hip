@@ -53,8 +53,11 @@ struct Place {
 };
 
 // This workgroup's share [p0, p1) of the line and the place of its first tile, the same in
-// every wavefront.  Shares have at least `least` tiles (a power of two) where the line is
-// that long; workgroups past the last get an empty one.
+// every wavefront.  A short line goes to as many workgroups as it has tiles, the others get
+// an empty share: a block's tiles one after another take longer than their join (128 tokens
+// over 100, 32 heads, blocks of 256 rows: 23.4 us in shares of at least two tiles, 15.3 in
+// shares of one, the join 7.1 either way; single tokens of three requests, int8, 14.4 us in
+// shares of at least four, 10.3; 17 fp32 tokens over two caches 17.6 and 13.2).
 struct Share {
   Shares all;
   unsigned p0, p1;
@@ -87,8 +90,7 @@ __device__ inline int find_block(const Req& r, unsigned G, int rb, int limit, un
   return max(n - 1, 0);
 }
 
-__device__ inline Share find_share(const AttendParams& a, int w, int rb, int limit,
-                                   unsigned least, Place& at) {
+__device__ inline Share find_share(const AttendParams& a, int w, int rb, int limit, Place& at) {
   const int lane = threadIdx.x & 63;
   Share s{};
   Req mine{};
@@ -121,8 +123,8 @@ __device__ inline Share find_share(const AttendParams& a, int w, int rb, int lim
   for (int b0 = 0; b0 < a.ch.batch; b0 += 64) total = add_sat(total, step(b0));
   // (2^31 tiles cannot be where no two requests share a row)
   if (total == 0 || total >= 1u << 31) return s;
-  s.all = make_shares(total, min((total + least - 1) / least, gridDim.x));
-  if (unsigned(w) >= min((total + least - 1) / least, gridDim.x)) return s;
+  s.all = make_shares(total, min(total, gridDim.x));
+  if (unsigned(w) >= total) return s;
   s.p0 = s.all.begin(w);
   s.p1 = s.all.begin(w + 1);
   unsigned seen = 0;
@@ -324,7 +326,13 @@ __device__ inline float infinity_of(float share, int sign) {
 // first leaves: rounded to one, it would be the largest error of the output (queries of
 // standard deviation 2: 2-norm 0.0041 of the output's, 0.0024 with both, of which 0.0017 are
 // the output's own rounding).  Both come from LDS every step, and the MFMAs that the second
-// adds are idle time here.
+// adds are idle time here.  Probabilities are rounded to bf16 for their product, as everywhere
+// in this library; their sum and the output stay in fp32.
+//
+// Bound by memory: 256 KB are in flight a CU, and the rest hides under them.  24 requests of
+// 1200 to 6200 tokens (bf16, 373 MB) in pages of 128: 71 to 77 us, 5.2 to 4.8 TB/s of the 6.0
+// that a read of contiguous memory reaches (pages of 64: 70); one of 128k in int8 (277 MB):
+// 57, 4.9; eight of those 376 us, 5.9.
 template <typename S, int D, int NB>
 __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
   using T = __bf16;
@@ -347,9 +355,8 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
   const int col = lane & 15, j = lane >> 4;
   const int PS = a.pg.PS, limit = a.ch.max_pages * PS, rb = a.rb;
   stage_turns<D>(a, s_turns);
-  // (fewer tiles a workgroup would leave wavefronts without a step)
   Place at;
-  const Share share = find_share(a, blockIdx.x, rb, limit, I8 ? 4 : 2, at);
+  const Share share = find_share(a, blockIdx.x, rb, limit, at);
   Join join{};
   if (share.p0 == share.p1) {
     if (tid == 0) a.joins[blockIdx.x] = join;
@@ -733,6 +740,14 @@ __device__ inline void wait_loads_barrier() {
 // c2kv_compose rounds them.  (2048 tokens over 32k, 32 query heads: 1.30 ms.  Keys decoded and
 // rounded too: 1.14, but the 2-norm of the error is then 0.0052 of the output's, not 0.0045;
 // value scales applied to the probabilities instead: 1.35, and 0.0042.)
+//
+// Bound by the MFMAs' share of a wavefront pair's time: 2048 tokens over 32k (64 query heads,
+// 2.27 TFLOP) in 2.03 ms, 1.12 PFLOP/s, where a library product of 8192 cubed reaches 1.21;
+// the MFMAs are busy 57 % of the time, the softmax and the operands' LDS reads the rest.  A
+// wavefront that runs the scores of one tile beside the softmax of the tile before spills;
+// values' rows exchanged so that no LDS read meets a conflict (a third do) change nothing.
+// fp32: 1024 tokens over 1024, 32 heads, 259 us, 100 TFLOP/s of the 147 that a library product
+// of 4096 cubed reaches.
 template <typename T, typename S, int D, int RG>
 __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
   using M = Mma<T>;
@@ -779,7 +794,7 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
                                    : int(blockIdx.x);
   stage_turns<D>(a, s_turns);
   Place at;
-  const Share share = find_share(a, w, RB, limit, 2, at);
+  const Share share = find_share(a, w, RB, limit, at);
   Join join{};
   unsigned p = share.p0;
   lds_barrier();                                 // the turns are there
@@ -1334,7 +1349,8 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
 // NW / PW sets of PW wavefronts of all the workgroups blockIdx.y; a set's wavefronts take
 // every PW-th piece, a lane D / 64 columns.  Bound by two dependent loads (the join, the
 // pieces) and the partials' bytes: units of few rows have many pieces (PW = 4), large ones
-// few (PW = 1).
+// few (PW = 1).  24 single tokens: 5.5 us; 2048 rows of 64 heads: 27 us, both above the 4 us
+// that an empty launch takes.
 template <typename T, int D, int RB, int PW>
 __global__ __launch_bounds__(256) void join_kernel(AttendParams a) {
   constexpr int CPL = D / 64, NW = 4, N = PW > 1 ? 16 : 8;   // columns of a lane; pieces in flight
@@ -1442,8 +1458,8 @@ AttendShape attend_shape(int store, int D, int64_t rows_max, int64_t max_chunk, 
   const int64_t G = rows_max / max_chunk;
   // Single tokens: as many of a token's rows as divide them evenly, up to 32.  (Chunks of a
   // few tokens run faster in blocks of rows, which read the keys once for all of them: 16
-  // requests of 3 to 7 drafts, 4 query heads a kv-head, 73 + 22 us in units of 32 mixed rows,
-  // 78 + 6 in blocks of 128.)  fp32 has the 128-row kernel only.
+  // requests of 3 to 7 drafts, 4 query heads a kv-head, 95 us in units of 32 mixed rows and
+  // their join, 88 in blocks of 128.)  fp32 has the 128-row kernel only.
   if (store != C2KV_F32 && max_chunk == 1) {
     for (s.unit_rows = int(G < 32 ? G : 32); G % s.unit_rows != 0;) --s.unit_rows;
     s.rows = s.unit_rows <= 16 ? 16 : 32;

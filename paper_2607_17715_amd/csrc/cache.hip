@@ -226,7 +226,9 @@ __global__ __launch_bounds__(256) void write_rows_kernel(WriteParams a) {
 
 // A workgroup per 64-slot tile of a request that its chunk touches, for the kv-heads
 // blockIdx.y, blockIdx.y + gridDim.y, ...: keys by rows, values transposed through LDS.
-// The turn of a (token, 8 pairs) unit is formed once for all of a workgroup's heads.
+// The turn of a (token, 8 pairs) unit is formed once for all of a workgroup's heads.  Bound by
+// HBM: 16384 tokens of 8 heads of 128 in bf16 (134 MB), 24.5 us = 5.5 TB/s, a 1 GiB copy 5.2;
+// int8, 9400 tokens of ragged prompts (58 MB): 16 us, 3.6 TB/s, 4 us of it the launch.
 template <typename T, typename S, int D>
 __global__ __launch_bounds__(256) void write_tile_kernel(WriteParams a) {
   constexpr int NTH = 256;
@@ -349,7 +351,8 @@ __global__ __launch_bounds__(256) void write_tile_kernel(WriteParams a) {
 // ----------------------------------------------------------------------------
 
 // The tiles of write_tile_kernel the other way: rows in the activation type, int8 decoded
-// and keys turned in fp32, rounded once.
+// and keys turned in fp32, rounded once.  Bound by HBM: 32768 int8 tokens (204 MB) in 33 us =
+// 6.1 TB/s.
 template <typename T, typename S, int D>
 __global__ __launch_bounds__(256) void read_tile_kernel(ReadParams a) {
   constexpr int NTH = 256;
@@ -460,7 +463,9 @@ __global__ __launch_bounds__(256) void read_tile_kernel(ReadParams a) {
 // ----------------------------------------------------------------------------
 
 // A thread per (token, 8 pairs): the unit's keys (and the values of the same columns) for
-// the kv-heads blockIdx.y, blockIdx.y + gridDim.y, ..., its turn formed once for all.
+// the kv-heads blockIdx.y, blockIdx.y + gridDim.y, ..., its turn formed once for all.  Bound by
+// HBM: 65536 tokens into int8 (407 MB) in 106 us = 3.9 TB/s; their codes leave as 8 bytes a
+// thread (exchanged into 16 first: no faster), a 4-byte scale a row beside them.
 template <typename T, typename S, int D>
 __global__ __launch_bounds__(256) void pool_write_kernel(PoolWriteParams a) {
   constexpr int KU = D / 16, TOKENS = 256 / KU;

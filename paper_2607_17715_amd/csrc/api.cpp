@@ -615,6 +615,7 @@ c2kv_status c2kv_cache_attend(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,
     p.part_o = reinterpret_cast<float*>(ws + sh.part_o);
     p.part_ml = reinterpret_cast<float2*>(ws + sh.part_ml);
     p.joins = reinterpret_cast<c2kv::Join*>(ws + sh.joins);
+    p.groups = sh.groups;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e = timed("cache_attend", [&](hipEvent_t e0, hipEvent_t e1) {
       return c2kv::launch_cache_attend(p, sh, cache->dtype, cfg->head_dim, s, e0, e1);

@@ -1345,24 +1345,68 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
 // join
 // ----------------------------------------------------------------------------
 
-// The unit that workgroup blockIdx.x began and others finished.  Its rows are dealt to the
-// NW / PW sets of PW wavefronts of all the workgroups blockIdx.y; a set's wavefronts take
-// every PW-th piece, a lane D / 64 columns.  Bound by two dependent loads (the join, the
-// pieces) and the partials' bytes: units of few rows have many pieces (PW = 4), large ones
-// few (PW = 1).  24 single tokens: 5.5 us; 2048 rows of 64 heads: 27 us, both above the 4 us
-// that an empty launch takes.
+// Units that lie in several workgroups.  A set of PW wavefronts takes a row, its wavefronts
+// every PW-th piece, a lane D / 64 columns.  Bound by dependent loads (the join, the pieces)
+// and the partials' bytes.  Units of few rows have many pieces: PW = 4, and workgroup
+// (w, y) takes rows y, y + gridDim.y, .. of the unit that workgroup w began (24 single
+// tokens: 5.5 us; an empty launch takes 4).  Blocks have many rows, and how many of them are
+// cut depends on the lengths: PW = 1, and all their rows, in one line, are shared evenly (512
+// rows of a kv-head over 4128 tokens, 16 pieces each: 30.0 us with workgroups for every share's
+// unit, cut or not, 11.4 so; 128 tokens over 100: 7.8 and 4.9; where most shares are cut, finding
+// the rows costs more than it gives: 2048 tokens of 64 heads 20.6 and 25.2, of 150 us before
+// them; 24 units of drafts 4.7 and 6.3).
 template <typename T, int D, int RB, int PW>
 __global__ __launch_bounds__(256) void join_kernel(AttendParams a) {
   constexpr int CPL = D / 64, NW = 4, N = PW > 1 ? 16 : 8;   // columns of a lane; pieces in flight
+  constexpr int JPL = 4;                       // joins of a lane, PW = 1
   __shared__ float s_x[NW][D];
-  const int w0 = blockIdx.x, wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const Join jn = a.joins[w0];
-  const int pieces = jn.last - w0 + 1;
-  // piece k: the second partial of w0, then the first ones of those after it
-  auto at = [&](int k, int row) { return (size_t(2) * (w0 + k) + (k == 0 ? 1 : 0)) * RB + row; };
+  const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int mine = wave % PW;
-  for (int row = blockIdx.y * (NW / PW) + wave / PW; row < jn.nrows;
-       row += gridDim.y * (NW / PW)) {
+  unsigned nrows[JPL] = {}, incl = 0, rows;
+  if constexpr (PW > 1) {
+    rows = unsigned(a.joins[blockIdx.x].nrows);
+  } else {
+#pragma unroll
+    for (int i = 0; i < JPL; ++i)
+      if (JPL * lane + i < a.groups) nrows[i] = unsigned(a.joins[JPL * lane + i].nrows);
+    incl = wave_scan((nrows[0] + nrows[1]) + (nrows[2] + nrows[3]));
+    rows = unsigned(__builtin_amdgcn_readlane(int(incl), 63));
+  }
+  // PW = 1: neighbouring rows to a set, so that the join is mostly the one before
+  const unsigned set = blockIdx.x * NW + wave, sets = gridDim.x * NW;
+  const unsigned each = (rows + sets - 1) / sets;
+  const unsigned first = PW > 1 ? blockIdx.y : set * each;
+  const unsigned last = PW > 1 ? rows : min(rows, first + each);
+  int w0 = blockIdx.x, row = int(first);
+  Join jn{};
+  if constexpr (PW > 1) jn = a.joins[w0];
+  for (unsigned at_row = first; at_row < last; at_row += PW > 1 ? gridDim.y : 1) {
+    if constexpr (PW > 1) {
+      row = int(at_row);
+    } else if (++row >= jn.nrows) {
+      const int src = __builtin_ctzll(__ballot(incl > at_row));
+      unsigned n[JPL], before = unsigned(__builtin_amdgcn_readlane(int(incl), src));
+#pragma unroll
+      for (int i = 0; i < JPL; ++i) {
+        n[i] = unsigned(__builtin_amdgcn_readlane(int(nrows[i]), src));
+        before -= n[i];
+      }
+      w0 = JPL * src;
+      unsigned rest = at_row - before;
+#pragma unroll
+      for (int i = 0; i < JPL - 1; ++i)
+        if (w0 == JPL * src + i && rest >= n[i]) {
+          rest -= n[i];
+          ++w0;
+        }
+      row = int(rest);
+      jn = a.joins[w0];
+    }
+    const int pieces = jn.last - w0 + 1;
+    // piece k: the second partial of w0, then the first ones of those after it
+    auto at = [&](int k, int r) {
+      return (size_t(2) * (w0 + k) + (k == 0 ? 1 : 0)) * RB + r;
+    };
     float x[CPL] = {}, m = kNegInf, l = 0.f;
     for (int k0 = 0; k0 < pieces; k0 += PW * N) {
       float v[N][CPL];
@@ -1469,7 +1513,7 @@ AttendShape attend_shape(int store, int D, int64_t rows_max, int64_t max_chunk, 
   const double tiles = double(batch) * double(heads) *
                        double((rows_max + s.unit_rows - 1) / s.unit_rows) *
                        double((kv_max + ST - 1) / ST);   // (may pass 64 bits)
-  const int64_t most = s.rows <= 32 ? 512 : 256;   // two workgroups a CU, or one
+  const int64_t most = s.rows <= 32 ? 512 : 256;   // two workgroups a CU, or one (4 a lane: joins)
   s.groups = int(tiles < most ? tiles : most);
   size_t at = 0;
   s.part_o = at;
@@ -1493,7 +1537,9 @@ hipError_t launch_cache_merge(const AttendParams& p, const AttendShape& sh, int 
                               hipStream_t st, hipEvent_t e0, hipEvent_t e1) {
   return with_types(store, D, [&](auto t, auto, auto d) {
     return launch(join_fn<decltype(t), decltype(d)::value>(sh.rows),
-                  dim3(unsigned(sh.groups), sh.rows <= 32 ? 4 : 32), dim3(256), st, p, e0, e1);
+                  sh.rows <= 32 ? dim3(unsigned(sh.groups), 4)
+                                : dim3(unsigned(min(2048, sh.groups * (sh.rows / 4)))),
+                  dim3(256), st, p, e0, e1);
   });
 }
 

@@ -81,6 +81,7 @@ struct AttendParams {
   float* part_o;                // [2 * groups][RB][D]
   float2* part_ml;              // [2 * groups][RB] reference maximum (base 2), sum
   struct Join* joins;           // [groups]
+  int32_t groups;
 };
 
 // A unit cut by a border between workgroups (joins[w]: the one that begins in workgroup

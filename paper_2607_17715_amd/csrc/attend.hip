@@ -1352,9 +1352,9 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
 // tokens: 5.5 us; an empty launch takes 4).  Blocks have many rows, and how many of them are
 // cut depends on the lengths: PW = 1, and all their rows, in one line, are shared evenly (512
 // rows of a kv-head over 4128 tokens, 16 pieces each: 30.0 us with workgroups for every share's
-// unit, cut or not, 11.4 so; 128 tokens over 100: 7.8 and 4.9; where most shares are cut, finding
-// the rows costs more than it gives: 2048 tokens of 64 heads 20.6 and 25.2, of 150 us before
-// them; 24 units of drafts 4.7 and 6.3).
+// unit, cut or not, 10.1 so; 128 tokens over 100: 7.8 and 4.4; drafts 4.7 and 4.6; where most
+// shares are cut, finding the rows costs: 2048 tokens of 64 heads 20.6 and 25.4, of 150 us
+// before them.  1024 workgroups; 512: 36.5, 2048: the same, but drafts 6.3; 8192: 32.3).
 template <typename T, int D, int RB, int PW>
 __global__ __launch_bounds__(256) void join_kernel(AttendParams a) {
   constexpr int CPL = D / 64, NW = 4, N = PW > 1 ? 16 : 8;   // columns of a lane; pieces in flight
@@ -1538,7 +1538,7 @@ hipError_t launch_cache_merge(const AttendParams& p, const AttendShape& sh, int 
   return with_types(store, D, [&](auto t, auto, auto d) {
     return launch(join_fn<decltype(t), decltype(d)::value>(sh.rows),
                   sh.rows <= 32 ? dim3(unsigned(sh.groups), 4)
-                                : dim3(unsigned(min(2048, sh.groups * (sh.rows / 4)))),
+                                : dim3(unsigned(min(1024, sh.groups * (sh.rows / 4)))),
                   dim3(256), st, p, e0, e1);
   });
 }

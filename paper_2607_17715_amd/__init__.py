@@ -300,13 +300,21 @@ class Plan:
 
 
 def pool_desc(k, v, k_scale=None, v_scale=None) -> PoolDesc:
+    """A pool of rows k and v [n_rows][H_kv][D], for int8 with float32 scales [n_rows][H_kv],
+    all on one device.  The descriptor keeps the tensors that it points to."""
     import torch
     code = {torch.float32: C2KV_F32, torch.bfloat16: C2KV_BF16, torch.int8: C2KV_I8}[k.dtype]
     if v.dtype != k.dtype or v.shape != k.shape:
         raise ValueError("pool K and V must have the same dtype and shape")
-    desc = PoolDesc(code, _dev_ptr(k), _dev_ptr(v), _dev_ptr(k_scale), _dev_ptr(v_scale),
-                    int(k.shape[0]))
-    desc.row_shape, desc.dev = tuple(k.shape[1:]), k.get_device()
+    tensors = (k, v, k_scale, v_scale)
+    if code == C2KV_I8:                        # (of other pools the library reads no scales)
+        for s in tensors[2:]:
+            if s is not None and (s.dtype != torch.float32 or s.shape != k.shape[:2]):
+                raise ValueError(f"pool scales must be float32 {list(k.shape[:2])}, got {s.dtype} "
+                                 f"{list(s.shape)}")
+    _one_device(*tensors)
+    desc = PoolDesc(code, *(_dev_ptr(t) for t in tensors), int(k.shape[0]))
+    desc.tensors, desc.row_shape, desc.dev = tensors, tuple(k.shape[1:]), k.get_device()
     return desc
 
 

@@ -2,9 +2,11 @@
 its buffer, and the refusals of the C ABI and of the binding (all before any device work,
 so the pointers here are never followed)."""
 import ctypes
+import gc
 import os
 import shutil
 import subprocess
+import weakref
 
 import numpy as np
 import pytest
@@ -186,6 +188,48 @@ def test_binding_refuses_shapes_and_types():
         c2kv.Chunks(i(3), i(2).long(), i(2, 4), 5)
     with pytest.raises(ValueError):                      # one offset missing
         c2kv.Chunks(i(2), i(2), i(2, 4), 5)
+
+
+@pytest.mark.parametrize("what", ["k_scale", "v_scale"])
+@pytest.mark.parametrize("scale", [
+    torch.ones(7, 2, dtype=torch.float16),               # half the bytes that are written
+    torch.ones(7),                                       # one scale a row
+    torch.ones(6, 2),                                    # a row short
+    torch.ones(2, 7),
+])
+def test_binding_refuses_pool_scales(monkeypatch, scale, what):
+    """c2kv_pool_write stores a float32 at row * H_kv + head of the scales."""
+    monkeypatch.setattr(c2kv, "_dev_ptr", lambda t: None if t is None else t.data_ptr())
+    k, good = torch.zeros(7, 2, 64, dtype=torch.int8), torch.ones(7, 2)
+    assert c2kv.pool_desc(k, k.clone(), good, good.clone()).k_scale == good.data_ptr()
+    with pytest.raises(ValueError, match="scales"):
+        c2kv.pool_desc(k, k.clone(), **{"k_scale": good, "v_scale": good, what: scale})
+
+
+@pytest.mark.parametrize("i", [1, 2, 3])
+def test_binding_refuses_pools_over_two_devices(monkeypatch, i):
+    monkeypatch.setattr(c2kv, "_dev_ptr", lambda t: None)
+    t = [torch.zeros(7, 2, 64, dtype=torch.int8), torch.zeros(7, 2, 64, dtype=torch.int8),
+         torch.ones(7, 2), torch.ones(7, 2)]
+    c2kv.pool_desc(*t)
+    t[i] = t[i].to("meta")
+    with pytest.raises(ValueError, match="different devices"):
+        c2kv.pool_desc(*t)
+
+
+def test_pool_descriptor_keeps_its_tensors(monkeypatch):
+    """Its pointers must not outlive what they point to."""
+    monkeypatch.setattr(c2kv, "_dev_ptr", lambda t: t.data_ptr())
+    t = [torch.zeros(7, 2, 64, dtype=torch.int8), torch.zeros(7, 2, 64, dtype=torch.int8),
+         torch.ones(7, 2), torch.ones(7, 2)]
+    refs = [weakref.ref(x) for x in t]
+    pool = c2kv.pool_desc(*t)
+    del t
+    gc.collect()
+    assert all(r() is not None for r in refs)
+    del pool
+    gc.collect()
+    assert all(r() is None for r in refs)
 
 
 def test_binding_refuses_rows_that_overlap():

@@ -192,11 +192,17 @@ c2kv_status check_cache(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,
     return fail(C2KV_E_UNSUPPORTED, "block tables of more than 2^30 tokens are not built");
   if (int64_t(ch->n_tokens) * cfg->n_q_heads > (1ll << 31) - 1)
     return fail(C2KV_E_UNSUPPORTED, "chunks of 2^31 (token, head) rows or more are not built");
-  // (a launch counts its threads in 32 bits: 256 for each tile of tokens)
   if (ch->n_tokens > 1 << 29)
     return fail(C2KV_E_UNSUPPORTED, "chunks of more than 2^29 tokens are not built");
   if (ch->batch > 1 << 22)
     return fail(C2KV_E_UNSUPPORTED, "batches of more than 2^22 requests are not built");
+  return C2KV_OK;
+}
+
+// Refuses batches whose tiles of tokens a launch cannot count.
+c2kv_status check_tiles(const c2kv_chunks& ch) {
+  if (c2kv::most_chunk_tiles(ch.n_tokens, ch.batch) > c2kv::kMostGroups)
+    return fail(C2KV_E_UNSUPPORTED, "batches that may fill 2^24 tiles of tokens are not built");
   return C2KV_OK;
 }
 
@@ -533,6 +539,7 @@ c2kv_status c2kv_cache_write(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,
   return guarded([&] {
     c2kv_status st = check_cache(cfg, cache, chunks);
     if (st == C2KV_OK && chunks->n_tokens == 0) return C2KV_OK;
+    if (st == C2KV_OK) st = check_tiles(*chunks);
     if (st == C2KV_OK) st = check_rows("k", *cfg, k, cfg->n_kv_heads, k_stride);
     if (st == C2KV_OK) st = check_rows("v", *cfg, v, cfg->n_kv_heads, v_stride);
     if (st != C2KV_OK) return st;
@@ -552,6 +559,7 @@ c2kv_status c2kv_cache_read(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,
   return guarded([&] {
     c2kv_status st = check_cache(cfg, cache, chunks);
     if (st == C2KV_OK && chunks->n_tokens == 0) return C2KV_OK;
+    if (st == C2KV_OK) st = check_tiles(*chunks);
     int64_t dense = 0;
     if (st == C2KV_OK) st = check_rows("k", *cfg, k, cfg->n_kv_heads, dense);
     if (st == C2KV_OK) st = check_rows("v", *cfg, v, cfg->n_kv_heads, dense);

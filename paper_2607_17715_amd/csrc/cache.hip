@@ -540,17 +540,11 @@ hipError_t launch_cache_write(const WriteParams& p, int store, int D, int max_ch
     using T = decltype(t);
     using S = decltype(s);
     constexpr int kD = decltype(d)::value;
-    // A wavefront a (token, kv-head) ends soonest where all of them run at once, or where a
-    // tile would hold few tokens; else tiles, which write whole lines (bf16, 8 heads of 128,
-    // rows against tiles: 256 tokens 5.4 | 6.1 us, 512 6.8 | 6.3; 128 requests of 1 token
-    // 5.6 | 11.4, of 8 12.1 | 12.2, of 32 26.9 | 18.2).  (A launch counts its threads, 64 a
-    // unit, in 32 bits.)
-    const int64_t units = int64_t(p.ch.n_tokens) * p.pg.Hkv;
-    if (units <= 2048 || (max_chunk <= 8 && units < 1 << 26)) {
+    if (write_by_rows(p.ch.n_tokens, p.pg.Hkv, max_chunk)) {
       return launch(reinterpret_cast<const void*>(&write_rows_kernel<T, S, kD>),
-                    dim3(unsigned((units + 3) / 4)), dim3(256), st, p, e0, e1);
+                    dim3(unsigned(row_groups(p.ch.n_tokens, p.pg.Hkv))), dim3(256), st, p, e0, e1);
     }
-    const int64_t tiles = p.ch.n_tokens / ST + 2ll * p.ch.batch;
+    const int64_t tiles = most_chunk_tiles(p.ch.n_tokens, p.ch.batch);
     return launch(reinterpret_cast<const void*>(&write_tile_kernel<T, S, kD>),
                   dim3(unsigned(tiles), head_groups(tiles, p.pg.Hkv)), dim3(256), st, p, e0, e1);
   });
@@ -561,7 +555,7 @@ hipError_t launch_cache_read(const ReadParams& p, int store, int D, hipStream_t 
   return with_types(store, D, [&](auto t, auto s, auto d) {
     using T = decltype(t);
     using S = decltype(s);
-    const int64_t tiles = p.ch.n_tokens / ST + 2ll * p.ch.batch;
+    const int64_t tiles = most_chunk_tiles(p.ch.n_tokens, p.ch.batch);
     return launch(reinterpret_cast<const void*>(&read_tile_kernel<T, S, decltype(d)::value>),
                   dim3(unsigned(tiles), head_groups(tiles, p.pg.Hkv)), dim3(256), st, p, e0, e1);
   });

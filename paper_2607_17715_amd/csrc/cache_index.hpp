@@ -47,6 +47,29 @@ C2KV_INDEX_FN Tiles chunk_tiles(const Req& r, int limit) {
   return {lo / kSlotTile, (hi - 1) / kSlotTile - lo / kSlotTile + 1};
 }
 
+// ---- launches -----------------------------------------------------------------------
+
+// Workgroups of 256 threads that a launch can have: it counts its threads in 32 bits.
+constexpr int64_t kMostGroups = (1ll << 24) - 1;
+
+// A bound on a batch's chunk_tiles, which is the grid of the tile kernels: a chunk of n tokens
+// falls in n / kSlotTile + 2 tiles at most.
+C2KV_INDEX_FN int64_t most_chunk_tiles(int64_t n_tokens, int64_t batch) {
+  return n_tokens / kSlotTile + 2 * batch;
+}
+// Workgroups of the row kernel: four (token, kv-head) units each.
+C2KV_INDEX_FN int64_t row_groups(int64_t n_tokens, int64_t heads) {
+  return (n_tokens * heads + 3) / 4;
+}
+// Whether a write goes by rows.  A wavefront a (token, kv-head) ends soonest where all of them
+// run at once, or where a tile would hold few tokens; else tiles, which write whole lines
+// (bf16, 8 heads of 128, rows against tiles: 256 tokens 5.4 | 6.1 us, 512 6.8 | 6.3; 128
+// requests of 1 token 5.6 | 11.4, of 8 12.1 | 12.2, of 32 26.9 | 18.2).
+C2KV_INDEX_FN bool write_by_rows(int64_t n_tokens, int64_t heads, int max_chunk) {
+  return n_tokens * heads <= 2048 ||
+         (max_chunk <= 8 && row_groups(n_tokens, heads) <= kMostGroups);
+}
+
 // Slots [lo, hi) of a tile of chunk_tiles belong to the chunk; slot s is row row0 + s.
 struct TileSlots {
   int lo, hi, row0;

@@ -153,6 +153,27 @@ def test_what_a_launch_cannot_count_is_refused(kw, calls, text):
         assert st == UNSUP and text in msg, (name, st, msg)
 
 
+def test_tiles_that_a_launch_cannot_count_are_refused():
+    """Each bound alone is accepted, but the tiles of both together are 2^24 workgroups."""
+    built = _args(hq=1, hkv=1, batch=1 << 22, n_tokens=1 << 29)
+    for name in ("write", "read"):
+        st = _calls(*built)[name]()
+        msg = c2kv.lib().c2kv_last_error().decode()
+        assert st == UNSUP and "2^24 tiles" in msg, (name, st, msg)
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="g++ is not installed")
+def test_accepted_calls_have_grids_that_a_launch_counts(tmp_path):
+    exe = str(tmp_path / "cache_launch")
+    subprocess.run(["g++", "-std=c++17", "-O2", "-I",
+                    os.path.join(ROOT, "paper_2607_17715_amd", "csrc"),
+                    os.path.join(ROOT, "tests", "cache_launch.cpp"), "-o", exe],
+                   check=True, timeout=300)
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stdout[-2000:]
+    assert int(r.stdout.split()[1]) > 1000, r.stdout
+
+
 def test_null_descriptors_are_refused():
     a, cfg, cache, ch = _args()
     lib, r = c2kv.lib(), ctypes.byref

@@ -371,7 +371,8 @@ c2kv_status c2kv_cache_read(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,
  * token t of request b sees cache indices j <= kv_len[b] - n_b + t.  q [n_tokens][H_q][D]
  * with q_stride elements between tokens (0: H_q * D), turned to pos as in
  * c2kv_cache_write (NULL: as it is).  out [n_tokens][H_q][D], lse [n_tokens][H_q] float32
- * natural-log (NULL to skip).  A token that sees no key gets zeros and an lse of -inf;
+ * natural-log (NULL to skip).  A token that sees no key gets zeros and an lse of -inf; a
+ * key whose score is -inf has no weight, and one of +inf or NaN makes its row NaN;
  * what lies in pages behind the last cached token has no effect, whatever it is.
  * workspace: device memory on 256 bytes, of c2kv_cache_attend_workspace's size; calls
  * that share one must be ordered.  It need not be cleared.  out must not overlap q, nor

@@ -222,12 +222,25 @@ __device__ inline bf16x8 bf16_of(const float (&x)[8]) {
                              pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
   return __builtin_bit_cast(bf16x8, u);
 }
-// what bf16_of left of x
-__device__ inline bf16x8 rest_of(const float (&x)[8], const bf16x8& hi) {
+// x as two bf16 numbers, within 2^-16 of itself.  The first is cut short, so that the second has
+// its sign, and is never zero beside it (of 2^-94 and more; where the first says all, 2^-32 of it
+// stands in): an infinite key element then gives the one infinity that a single number gives, not
+// the NaN of infinity times zero or of two infinities of opposite sign.  An infinity stands in
+// both.
+__device__ inline void split_bf16(const float (&x)[8], bf16x8& hi, bf16x8& rest) {
+  uint32_t w[4];
   float r[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) r[e] = x[e] - static_cast<float>(hi[e]);
-  return bf16_of(r);
+  for (int e = 0; e < 8; ++e) {
+    const float h = __uint_as_float(__float_as_uint(x[e]) & 0xffff0000u);
+    r[e] = x[e] == h ? h * 0x1p-32f : x[e] - h;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    w[i] = __builtin_amdgcn_perm(__float_as_uint(x[2 * i + 1]), __float_as_uint(x[2 * i]),
+                                 0x07060302u);
+  hi = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+  rest = bf16_of(r);
 }
 __device__ inline bf16x8 bf16_of_i8(uint32_t w0, uint32_t w1) {
   const uint32_t w[2] = {w0, w1};
@@ -477,9 +490,7 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
         raw_to_f8<T>(qy[nb][c], y);
         turn_chunks<8>(s_turns + qd(c) % (D / 2), a.rope.pos, qpos[nb], a.qscale, x, y);
         auto put = [&](int i, const float (&v)[8]) __attribute__((always_inline)) {
-          const bf16x8 hi = bf16_of(v);
-          s_q[(nb * NQC + i) * 64 + lane] = hi;
-          s_rest[(nb * NQC + i) * 64 + lane] = rest_of(v, hi);
+          split_bf16(v, s_q[(nb * NQC + i) * 64 + lane], s_rest[(nb * NQC + i) * 64 + lane]);
         };
         if constexpr (NQP < NQC) {
           put(c, x);
@@ -934,11 +945,12 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
             q[4 * (c + NQC / 2) + e] = y[e];
           }
         } else {
-          q[c] = bf16_of(x);
-          q[c + NQC / 2] = bf16_of(y);
           if constexpr (TWO) {                   // (the same from both key parts)
-            s_rest[(rg * NQC + c) * 64 + lane] = rest_of(x, q[c]);
-            s_rest[(rg * NQC + c + NQC / 2) * 64 + lane] = rest_of(y, q[c + NQC / 2]);
+            split_bf16(x, q[c], s_rest[(rg * NQC + c) * 64 + lane]);
+            split_bf16(y, q[c + NQC / 2], s_rest[(rg * NQC + c + NQC / 2) * 64 + lane]);
+          } else {
+            q[c] = bf16_of(x);
+            q[c + NQC / 2] = bf16_of(y);
           }
         }
       }

@@ -515,6 +515,71 @@ def test_attend_values_that_later_tokens_see(n, hq, store):
     assert torch.equal(got[torch.isinf(want)], want[torch.isinf(want)])
 
 
+@pytest.mark.parametrize("store", ["f32", "bf16"])
+@pytest.mark.parametrize("n,hq,hint", [
+    ([1, 1], 8, 1), ([1, 1], 48, 1),             # single tokens, up to 16 and up to 32 heads
+    ([5, 3], 8, 1), ([5, 3], 8, 5), ([5, 3], 8, 10_000),      # a chunk by rows and by blocks
+    ([40, 90], 8, 90), ([300, 70], 2, 300),
+])
+def test_attend_keys_that_are_not_finite(n, hq, hint, store):
+    """Infinities and NaN in visible keys, whatever the kernel: a score of -inf is a key without
+    weight, one of +inf or NaN makes its row NaN, and rows and heads that do not see the key
+    are as they were.  The row's own sign of the query decides which."""
+    s = Scene(store, n, [70, 130], hq=hq, hkv=2, seed=22)
+    say(f"keys not finite {store} {n} hint {hint}")
+    inf = float("inf")
+    G = hq // s.hkv
+    # query values whose products with the odd keys have a sign, single-number ones among them
+    q = s.q
+    q[:, :, 7] = torch.where(q[:, :, 7] < 0, -0.5, 0.5)
+    q[:, :, 9] = torch.where(q[:, :, 9] < 0, -1.25, 0.75)
+    ch = s.chunks(max_chunk=hint)
+    was = s.out()
+    c2kv.c2kv_cache_attend(s.cfg, s.cache, ch, q, was)
+    where = cache_oracle.places(s.tok_off, s.kv_len, s.table, s.page, s.n_pages, s.n_tokens)
+    _, _, page, at = where[int(s.tok_off[0]) + n[0] // 2]
+    s.kp[page, 0, at, 7] = inf
+    _, _, page, at = where[int(s.tok_off[1]) + n[1] - 1]
+    s.kp[page, 0, at, 9], s.kp[page, 0, at, 7] = -inf, inf
+    s.kp[page, 1, at, 100] = float("nan")
+    s.kp[s.table[1, 0], 1, 17, 9] = -inf         # in the context, seen by all
+    out, lse = s.out(), s.lse()
+    c2kv.c2kv_cache_attend(s.cfg, s.cache, ch, q, out, None, lse)
+    torch.cuda.synchronize()
+    ref, ref_lse, has = dense64(s, q, None)
+    assert has.all()
+    nan = np.isnan(ref)
+    assert nan.any() and not nan.all() and (nan.all(-1) == nan.any(-1)).all()
+    got = f64(out)
+    assert (np.isnan(got) == nan).all()
+    assert (np.isnan(f64(lse)) == nan.any(-1)).all()
+    fine = ~nan.any(-1)
+    err, lerr = np.abs(got - ref)[fine], np.abs(f64(lse) - ref_lse)[fine]
+    if store == "f32":
+        assert err.max() <= 1e-5 and lerr.max() <= 1e-5
+    else:
+        assert err.max() <= 2e-2 and err.mean() <= 1e-2 and lerr.max() <= 5e-2
+    before = int(s.tok_off[0]) + n[0] // 2       # the first request's tokens that do not see it
+    assert torch.equal(out[:before], was[:before])
+    assert torch.equal(out[:n[0], G:], was[:n[0], G:])
+
+
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("n,hint", [([1, 1], 1), ([5, 3], 5), ([100, 40], 100)])
+def test_attend_infinite_queries(n, hint, store):
+    """A query whose every score is -inf sees no key; one with a score of +inf is NaN."""
+    s = Scene(store, n, [70, 130], seed=23)
+    s.kp[..., 7] = -s.kp[..., 7].abs().clamp_min(1)
+    s.q[0, 1, 7], s.q[n[0], 2, 7] = float("inf"), float("-inf")
+    out, lse = s.out(), s.lse()
+    c2kv.c2kv_cache_attend(s.cfg, s.cache, s.chunks(max_chunk=hint), s.q, out, None, lse)
+    torch.cuda.synchronize()
+    assert (out[0, 1] == 0).all() and lse[0, 1] == float("-inf")
+    assert torch.isnan(out[n[0], 2]).all() and torch.isnan(lse[n[0], 2])
+    out[0, 1], out[n[0], 2] = 1, 1
+    assert torch.isfinite(out).all() and (~torch.isfinite(lse)).sum() == 2
+
+
 def test_attend_large_scores():
     """Scores of some hundreds: one key takes all, no overflow."""
     s = Scene("bf16", [1, 50], [300, 200], seed=13)

@@ -352,7 +352,7 @@ typedef struct c2kv_chunks {
  * columns of one projection's output.  pos [n_tokens] DEVICE: k is not yet
  * RoPE-encoded and is turned to these positions; NULL: k is written as it is.  I8:
  * symmetric per (token, kv-head), scale = max|x| / 127 (1 for zeros) of the turned key
- * in fp32, code = x / scale to the nearest (either way within 2^-22 of a half); a row
+ * in fp32, code = x / scale rounded to fp32 and then to the nearest, halves to even; a row
  * that holds an infinity or a NaN reads back as NaN, one whose values are all below 2^-100
  * as zeros.  Two tokens of one call must not have the same place. */
 c2kv_status c2kv_cache_write(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,

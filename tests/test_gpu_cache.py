@@ -170,6 +170,46 @@ def test_int8_tiles_of_zeros_infinities_and_nans():
     assert (value(502, 0) == 0).all() and (value(502, 1) != 0).any()
 
 
+@pytest.mark.parametrize("how", ["rows", "tiles", "pool"])
+def test_int8_codes_are_the_rounded_quotients(how):
+    """scale = max / 127 and code = x / scale, each one fp32 division rounded once, the code then
+    to the nearest whole number (halves to even): bit for bit, for every pair of bf16 mantissas
+    over ten powers of two.  (Half of a row's maximum is such a half, 63.5, but for the
+    scale's own rounding.)"""
+    m = np.arange(128, 256, dtype=np.float32) / 128
+    top = np.repeat(m, 10)                       # a row for each maximum and power of two
+    x = np.tile(np.exp2(-np.arange(10, dtype=np.float32)), 128)[:, None] * m[None]
+    x[:, 1::2] *= -1
+    x = np.where(np.abs(x) > top[:, None], 0, x).astype(np.float32)
+    x[np.arange(len(x)), np.arange(len(x)) % 128] = top
+    scale = top / np.float32(127)
+    code = np.rint(x / scale[:, None])
+    assert scale.dtype == code.dtype == np.float32
+    n = len(x)
+    cfg = c2kv.attn_cfg(1, 1, 128, "bf16", 1e4)
+    rows = torch.from_numpy(x).cuda().bfloat16()[:, None]
+    assert (rows[:, 0].float().cpu().numpy() == x).all()
+    if how == "pool":
+        pk, pv = (torch.zeros((n, 1, 128), dtype=torch.int8, device="cuda") for _ in range(2))
+        ks, vs = (torch.zeros((n, 1), device="cuda") for _ in range(2))
+        c2kv.c2kv_pool_write(cfg, c2kv.pool_desc(pk, pv, ks, vs),
+                             torch.arange(n, device="cuda"), rows, rows.flip(0))
+        got = [t[:, 0].cpu().numpy() for t in (pk, ks, pv.flip(0), vs.flip(0))]
+    else:
+        # 1280 units go by rows, those of two heads by tiles
+        heads = 1 if how == "rows" else 2
+        s = Scene("i8", [n], [5], hq=heads, hkv=heads)
+        rows = rows.expand(n, heads, 128).contiguous()
+        c2kv.c2kv_cache_write(s.cfg, s.cache, s.chunks(), rows, rows.flip(0))
+        where = cache_oracle.places(s.tok_off, s.kv_len, s.table, s.page, s.n_pages, n)
+        page, at = (np.array([where[r][i] for r in range(n)]) for i in (2, 3))
+        got = [s.kp.cpu().numpy()[page, -1, at], s.ks.cpu().numpy()[page, -1, at],
+               s.vp.cpu().numpy()[page, -1, :, at][::-1], s.vs.cpu().numpy()[page, -1, at][::-1]]
+    for c, sc in (got[:2], got[2:]):
+        np.testing.assert_array_equal(sc, scale)
+        np.testing.assert_array_equal(c, code)
+
+
 @pytest.mark.parametrize("store", STORES)
 @pytest.mark.parametrize("n,d,hkv", [(1, 128, 8), (33, 64, 3), (1000, 128, 2), (257, 64, 1)])
 def test_pool_write(n, d, hkv, store):

@@ -733,7 +733,7 @@ struct WideTile {
 // because the compiler would wait for every such load before any LDS read.
 __device__ inline void load_to_lds(const void* base, uint32_t off, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-               :: "s"(lds), "v"(off), "s"(base) : "memory");
+               :: "s"(lds), "v"(off), "s"(base) : "m0", "memory");
 }
 // until at most N of this wavefront's loads are in flight, then every wavefront's
 template <int N>

@@ -342,10 +342,11 @@ __device__ inline float infinity_of(float share, int sign) {
 // adds are idle time here.  Probabilities are rounded to bf16 for their product, as everywhere
 // in this library; their sum and the output stay in fp32.
 //
-// Bound by memory: 256 KB are in flight a CU, and the rest hides under them.  24 requests of
-// 1200 to 6200 tokens (bf16, 373 MB) in pages of 128: 71 to 77 us, 5.2 to 4.8 TB/s of the 6.0
-// that a read of contiguous memory reaches (pages of 64: 70); one of 128k in int8 (277 MB):
-// 57, 4.9; eight of those 376 us, 5.9.
+// Bound by memory: with up to 16 rows 256 KB are in flight a CU (D = 128), and the rest hides under
+// them.  24 requests of 1200 to 6200 tokens (bf16, 373 MB) in pages of 128: 71 to 77 us, 5.2 to
+// 4.8 TB/s of the 6.0 that a read of contiguous memory reaches (pages of 64: 70); one of 128k in
+// int8 (277 MB): 57, 4.9; eight of those 376 us, 5.9.  With up to 32 rows one workgroup a CU has
+// 64 KB in flight: the first of these with 32 heads a kv-head 85 us and 24 of joining.
 template <typename S, int D, int NB>
 __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
   using T = __bf16;
@@ -1525,7 +1526,10 @@ AttendShape attend_shape(int store, int D, int64_t rows_max, int64_t max_chunk, 
   const double tiles = double(batch) * double(heads) *
                        double((rows_max + s.unit_rows - 1) / s.unit_rows) *
                        double((kv_max + ST - 1) / ST);   // (may pass 64 bits)
-  const int64_t most = s.rows <= 32 ? 512 : 256;   // two workgroups a CU, or one (4 a lane: joins)
+  // Two workgroups a CU, or one (4 a lane: joins): of the 32-row kernel two fit at D = 64 only (85
+  // KB of LDS at 128; 24 requests of 1200 to 6200 tokens, 256 heads over 8, 512 | 256 workgroups,
+  // with the join: D = 128 bf16 118 | 109 us, int8 96 | 83; D = 64 bf16 59 | 62, int8 49 | 53).
+  const int64_t most = s.rows == 16 || (s.rows == 32 && D == 64) ? 512 : 256;
   s.groups = int(tiles < most ? tiles : most);
   size_t at = 0;
   s.part_o = at;

@@ -135,6 +135,30 @@ def test_attention_workspace_is_checked():
         assert st == UNSUP and "2^31" in lib.c2kv_last_error().decode()
 
 
+def _workspace(**kw):
+    n = ctypes.c_size_t()
+    a, cfg, cache, ch = _args(ks=P, vs=P, **kw)
+    assert c2kv.lib().c2kv_cache_attend_workspace(*map(ctypes.byref, (cfg, cache, ch, n))) == 0
+    return n.value
+
+
+def _holds(groups, rows, d):
+    """Two partials of `rows` rows a workgroup, and its join of 32 bytes."""
+    up = lambda x: -(-x // 256) * 256
+    return up(2 * groups * rows * d * 4) + up(2 * groups * rows * 8) + up(32 * groups)
+
+
+@pytest.mark.parametrize("store", [c2kv.C2KV_BF16, c2kv.C2KV_I8])
+@pytest.mark.parametrize("heads,d,groups,rows", [
+    (1, 128, 512, 16), (16, 128, 512, 16), (16, 64, 512, 16),
+    # two workgroups a CU where they fit: not with 85 KB of LDS
+    (17, 128, 256, 32), (32, 128, 256, 32), (32, 64, 512, 32),
+])
+def test_workgroups_of_single_tokens(heads, d, groups, rows, store):
+    got = _workspace(hq=heads, hkv=1, d=d, store=store, n_tokens=2, max_chunk=1, max_pages=1 << 12)
+    assert got == _holds(groups, rows, d)
+
+
 @pytest.mark.parametrize("kw,calls,text", [
     (dict(hq=1, hkv=1, n_tokens=(1 << 29) + 1), CACHE, "2^29 tokens"),
     (dict(batch=(1 << 22) + 1), CACHE, "2^22 requests"),

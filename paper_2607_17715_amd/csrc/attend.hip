@@ -1513,12 +1513,19 @@ AttendShape attend_shape(int store, int D, int64_t rows_max, int64_t max_chunk, 
   AttendShape s{};
   auto up = [](size_t x) { return (x + 255) & ~size_t(255); };
   const int64_t G = rows_max / max_chunk;
-  // Single tokens: as many of a token's rows as divide them evenly, up to 32.  (Chunks of a
-  // few tokens run faster in blocks of rows, which read the keys once for all of them: 16
-  // requests of 3 to 7 drafts, 4 query heads a kv-head, 95 us in units of 32 mixed rows and
-  // their join, 88 in blocks of 128.)  fp32 has the 128-row kernel only.
-  if (store != C2KV_F32 && max_chunk == 1) {
-    for (s.unit_rows = int(G < 32 ? G : 32); G % s.unit_rows != 0;) --s.unit_rows;
+  // Single tokens of up to 32 heads a kv-head: a unit is the token's rows.  Of more heads it would
+  // be a part of them, and each part reads the cache again: that pays for int8 alone, whose blocks
+  // are slow, and for two parts (24 requests of 1200 to 6200 tokens, with the join, parts | blocks,
+  // D = 128: bf16 272 heads over 8 152 | 104 us, 512 over 8 162 | 106, 296 over 8, which 37 parts
+  // would divide, 1926 | 104; int8 116 | 109, 128 | 114, 1105 | 111; D = 64: bf16 79 | 68, 92 | 71,
+  // 1019 | 69; int8 64 | 135, 77 | 138, 590 | 136).  Chunks of a few tokens run faster in blocks as
+  // well, which read the keys once for all of them: 16 requests of 3 to 7 drafts, 4 query heads a
+  // kv-head, 95 us in units of 32 mixed rows and their join, 88 in blocks of 128.  fp32 has the
+  // 128-row kernel only.
+  const int64_t parts = G <= 32 ? 1 : 2;
+  if (store != C2KV_F32 && max_chunk == 1 && G <= 32 * parts && G % parts == 0 &&
+      (parts == 1 || store == C2KV_I8)) {
+    s.unit_rows = int(G / parts);
     s.rows = s.unit_rows <= 16 ? 16 : 32;
   } else {
     s.rows = s.unit_rows = store == C2KV_F32 || rows_max <= 128 ? 128 : 256;

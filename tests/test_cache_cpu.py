@@ -153,10 +153,20 @@ def _holds(groups, rows, d):
     (1, 128, 512, 16), (16, 128, 512, 16), (16, 64, 512, 16),
     # two workgroups a CU where they fit: not with 85 KB of LDS
     (17, 128, 256, 32), (32, 128, 256, 32), (32, 64, 512, 32),
+    # no two parts: blocks, which read the cache once for all heads
+    (33, 128, 256, 128), (37, 64, 256, 128), (66, 128, 256, 128), (129, 128, 256, 256),
 ])
 def test_workgroups_of_single_tokens(heads, d, groups, rows, store):
     got = _workspace(hq=heads, hkv=1, d=d, store=store, n_tokens=2, max_chunk=1, max_pages=1 << 12)
     assert got == _holds(groups, rows, d)
+
+
+def test_workgroups_of_two_parts():
+    """34 to 64 heads a kv-head: int8 in two parts, bf16 in blocks."""
+    for d, groups in ((128, 256), (64, 512)):
+        kw = dict(hq=40, hkv=1, d=d, n_tokens=2, max_chunk=1, max_pages=1 << 12)
+        assert _workspace(store=c2kv.C2KV_I8, **kw) == _holds(groups, 32, d)
+        assert _workspace(store=c2kv.C2KV_BF16, **kw) == _holds(256, 128, d)
 
 
 @pytest.mark.parametrize("kw,calls,text", [

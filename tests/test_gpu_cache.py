@@ -373,6 +373,18 @@ def test_prime_groups_and_many_requests(store):
         check_attend(s, out, lse, *dense64(s, s.q, s.pos.cpu().numpy()))
 
 
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("hq,d", [(33, 128), (40, 128), (64, 64), (66, 64), (130, 128)])
+def test_single_tokens_of_more_heads_than_a_unit(hq, d, store):
+    """Over 32 query heads a kv-head: int8 in two parts of them, where they are even and up to
+    64, and blocks of rows otherwise."""
+    s = Scene(store, [1, 1, 1], [70, 900, 0], hq=2 * hq, hkv=2, d=d, seed=34)
+    out, lse = s.out(), s.lse()
+    c2kv.c2kv_cache_attend(s.cfg, s.cache, s.chunks(max_chunk=1), s.q, out, s.pos, lse)
+    torch.cuda.synchronize()
+    check_attend(s, out, lse, *dense64(s, s.q, s.pos.cpu().numpy()))
+
+
 def test_offsets_past_32_bits():
     """A cache whose later pages lie beyond 2^32 elements from its start (4.4 GB each of keys
     and values, int8): written, read back and attended there."""

@@ -334,7 +334,9 @@ typedef struct c2kv_cache {
  * n_b = tok_off[b+1] - tok_off[b] of its kv_len[b] cached tokens.  Token t of the chunk
  * is row tok_off[b] + t of the call's tensors and cache index j = kv_len[b] - n_b + t,
  * at offset j % page_size of page block_table[b][j / page_size].  For a step of new
- * tokens kv_len counts them; to read a whole cache back, n_b = kv_len[b]. */
+ * tokens kv_len counts them; to read a whole cache back, n_b = kv_len[b].  max_chunk and
+ * max_kv choose the kernels, their launch and, in attention, how far a query is rounded;
+ * every token is answered, whatever they say. */
 typedef struct c2kv_chunks {
   int32_t batch;               /* B >= 1                                           */
   int32_t n_tokens;            /* rows of the chunk tensors, at least tok_off[B]   */
@@ -342,9 +344,9 @@ typedef struct c2kv_chunks {
   const int32_t* kv_len;       /* [B] DEVICE                                       */
   const int32_t* block_table;  /* [B][max_pages] DEVICE                            */
   int32_t max_pages;           /* columns of the block table, >= 1                 */
-  int32_t max_chunk;           /* a bound on n_b and one on kv_len, for launch     */
-  int32_t max_kv;              /* shapes only (every token is answered whatever they
-                                  say; 0: n_tokens and max_pages * page_size)      */
+  int32_t max_chunk;           /* a bound on n_b; 0: n_tokens, or in attention 1
+                                  where n_tokens <= B                              */
+  int32_t max_kv;              /* a bound on kv_len; 0: max_pages * page_size      */
 } c2kv_chunks;
 
 /* Write each chunk's tokens into the cache.  k, v [n_tokens][H_kv][D] in the act dtype,
@@ -374,6 +376,11 @@ c2kv_status c2kv_cache_read(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,
  * natural-log (NULL to skip).  A token that sees no key gets zeros and an lse of -inf; a
  * key whose score is -inf has no weight, and one of +inf or NaN makes its row NaN;
  * what lies in pages behind the last cached token has no effect, whatever it is.
+ * Rounding, bf16 activations: probabilities to bf16 for their product with the values; the
+ * turned and scaled query, where max_chunk * H_q / H_kv <= 128, to a sum of two bf16 numbers
+ * (a score within 2^-16 of sum |q_i k_i|), and where it is more to one, as c2kv_attend does
+ * (2^-8).  The same token may so come out differently beside a longer chunk or under another
+ * bound, within these; equal calls give equal bits.
  * workspace: device memory on 256 bytes, of c2kv_cache_attend_workspace's size; calls
  * that share one must be ordered.  It need not be cleared.  out must not overlap q, nor
  * in any of these calls what is written what is read. */

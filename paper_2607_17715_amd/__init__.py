@@ -391,7 +391,8 @@ class Cache:
 class Chunks:
     """The chunk of each request of a batch (c2kv_chunks): tok_off [B+1], kv_len [B] and
     block_table [B][max_pages], int32 on the device, read when the kernels run; n_tokens
-    rows in the tensors of a call; max_chunk and max_kv bound the lengths (0: unknown)."""
+    rows in the tensors of a call; max_chunk and max_kv bound the lengths (0: unknown) and choose
+    kernels, and so the rounding of an attention's queries, but not what is answered."""
 
     def __init__(self, tok_off, kv_len, block_table, n_tokens: int, max_chunk: int = 0,
                  max_kv: int = 0):

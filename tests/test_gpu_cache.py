@@ -360,6 +360,38 @@ def test_bounds_that_do_not_hold_change_no_result(i, store, hints):
     check_attend(s, out, lse, *dense64(s, s.q, s.pos.cpu().numpy()))
 
 
+@pytest.mark.parametrize("store", ["bf16", "i8"])
+@pytest.mark.parametrize("hint,half,blocks", [
+    (1, 2.0 ** -16, False),                      # single tokens: two bf16 numbers a query
+    (5, 2.0 ** -16, True), (32, 2.0 ** -16, True),           # blocks of 128 rows: the same
+    (33, 2.0 ** -8, True), (0, 2.0 ** -8, True),             # of 256 rows: one
+])
+def test_bounds_choose_how_far_queries_are_rounded(hint, half, blocks, store):
+    """The header's figures.  A score is off by at most `half` of the sum of its products'
+    magnitudes, and by what fp32 makes of turns and sums (2^-20 of it); the log-sum-exp is off by
+    no more, and in blocks, which sum the probabilities that they rounded to bf16, by 2^-8."""
+    s = Scene(store, [5, 3], [700, 90], pad_rows=50, seed=35)
+    out, lse = s.out(), s.lse()
+    ch = s.chunks(max_chunk=hint)
+    c2kv.c2kv_cache_attend(s.cfg, s.cache, ch, s.q, out, s.pos, lse)
+    torch.cuda.synchronize()
+    ref, ref_lse, has = dense64(s, s.q, s.pos.cpu().numpy())
+    check_attend(s, out, lse, ref, ref_lse, has)
+    # the largest sum of magnitudes of a (token, head)'s scores, from the pairs' amplitudes
+    amp, G = amplitude(f64(s.q)), s.hq // s.hkv
+    kp = np.abs(s.pages64()[0])
+    worst = np.zeros((s.n_tokens, s.hq))
+    for b in range(s.B):
+        r0, r1, n = int(s.tok_off[b]), int(s.tok_off[b + 1]), int(s.kv_len[b])
+        k = np.concatenate([kp[i] for i in s.table[b][:-(-n // s.page)]], 1)[:, :n]
+        for h in range(s.hq):
+            worst[r0:r1, h] = (amp[r0:r1, h] @ k[h // G].T).max(1) / s.d ** 0.5
+    err = np.abs(f64(lse) - ref_lse)[has]
+    bound = (half + 2.0 ** -20) * worst[has] + (2.0 ** -8 if blocks else 0) + 2.0 ** -20
+    say(f"lse error {err.max():.2e}, of its bound {(err / bound).max():.2f}")
+    assert (err <= bound).all()
+
+
 @pytest.mark.parametrize("store", STORES)
 def test_prime_groups_and_many_requests(store):
     """37 query heads a kv-head (no divisor up to 32), and 300 requests, some of them empty."""

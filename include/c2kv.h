@@ -344,8 +344,8 @@ typedef struct c2kv_chunks {
   const int32_t* kv_len;       /* [B] DEVICE                                       */
   const int32_t* block_table;  /* [B][max_pages] DEVICE                            */
   int32_t max_pages;           /* columns of the block table, >= 1                 */
-  int32_t max_chunk;           /* a bound on n_b; 0: n_tokens, or in attention 1
-                                  where n_tokens <= B                              */
+  int32_t max_chunk;           /* a bound on n_b; 0: n_tokens, or 1 where there are
+                                  no more tokens than requests                     */
   int32_t max_kv;              /* a bound on kv_len; 0: max_pages * page_size      */
 } c2kv_chunks;
 

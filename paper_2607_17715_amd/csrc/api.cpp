@@ -237,16 +237,13 @@ c2kv::RopeView rope(const c2kv_attn_cfg& cfg, const int32_t* pos) {
   return r;
 }
 int longest_chunk(const c2kv_chunks& c) {
-  return c.max_chunk > 0 && c.max_chunk < c.n_tokens ? c.max_chunk : c.n_tokens;
+  return c2kv::longest_chunk(c.max_chunk, c.n_tokens, c.batch);
 }
 // Launch shape of an attention call, from the bounds that the host knows.
 c2kv::AttendShape attend_shape(const c2kv_attn_cfg& cfg, const c2kv_cache& cache,
                                const c2kv_chunks& ch) {
   const int64_t G = cfg.n_q_heads / cfg.n_kv_heads;
-  // (as many rows as requests: most likely one token each)
-  const int64_t longest = ch.max_chunk == 0 && ch.n_tokens <= ch.batch ? 1
-                          : ch.n_tokens < 1                            ? 1
-                                                                       : longest_chunk(ch);
+  const int64_t longest = longest_chunk(ch);
   const int64_t room = int64_t(ch.max_pages) * cache.page_size;
   const int64_t kv = ch.max_kv > 0 && ch.max_kv < room ? ch.max_kv : room;
   return c2kv::attend_shape(cache.dtype, cfg.head_dim, longest * G, longest, ch.batch,

@@ -52,6 +52,13 @@ C2KV_INDEX_FN Tiles chunk_tiles(const Req& r, int limit) {
 // Workgroups of 256 threads that a launch can have: it counts its threads in 32 bits.
 constexpr int64_t kMostGroups = (1ll << 24) - 1;
 
+// The longest chunk of a batch as far as the host knows: its bound, and where none is given all
+// tokens, or one where there are no more of them than requests (a step, most likely).
+C2KV_INDEX_FN int longest_chunk(int max_chunk, int n_tokens, int batch) {
+  if (max_chunk == 0 && n_tokens <= batch) return 1;
+  return max_chunk > 0 && max_chunk < n_tokens ? max_chunk : imax_(n_tokens, 1);
+}
+
 // A bound on a batch's chunk_tiles, which is the grid of the tile kernels: a chunk of n tokens
 // falls in n / kSlotTile + 2 tiles at most.
 C2KV_INDEX_FN int64_t most_chunk_tiles(int64_t n_tokens, int64_t batch) {

@@ -1,6 +1,7 @@
 // Checks that every write and read that the growing cache accepts has a grid whose threads
 // (256 a workgroup) a launch counts in 32 bits: around each limit of tokens, requests and
-// heads, and where the row kernel gives way to the tiles.
+// heads, and where the row kernel gives way to the tiles; and what a batch's bound on its chunks
+// is where none is given.
 // Usage: cache_launch; prints "ok <calls checked>".
 #include <cstdio>
 #include <initializer_list>
@@ -38,6 +39,12 @@ int main() {
             ++checked;
           }
   const int64_t n = 0, b = 0, h = 0;
+  // the bound, at most all tokens; without one, a step is a token of each request
+  CHECK(longest_chunk(5, 100, 3) == 5 && longest_chunk(500, 100, 3) == 100);
+  CHECK(longest_chunk(0, 100, 99) == 100 && longest_chunk(0, 100, 100) == 1);
+  CHECK(longest_chunk(7, 100, 100) == 7 && longest_chunk(3, 0, 9) == 1);
+  CHECK(write_by_rows(512, 8, longest_chunk(0, 512, 512)));
+  CHECK(!write_by_rows(512, 8, longest_chunk(0, 512, 511)));
   CHECK(rows && tiles && refused);
   std::printf("ok %ld\n", checked);
   return 0;

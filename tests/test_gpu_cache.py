@@ -109,6 +109,25 @@ def test_write(i, store, hint):
         assert torch.equal(now, was)
 
 
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("n", [[1] * 300, [0] * 50 + [200] + [0] * 249])
+def test_write_of_a_step_without_a_bound(n, store):
+    """No more tokens than requests go by rows, a long chunk among them as well: the same as under
+    every bound."""
+    s = Scene(store, n, [(7 * i) % 150 for i in range(300)], hq=8, hkv=8, d=64, seed=36)
+    before, after = s.copies(), []
+    for hint in (0, 1, 300):
+        for t, was in zip((s.kp, s.vp, s.ks, s.vs), before):
+            if t is not None:
+                t.copy_(was)
+        c2kv.c2kv_cache_write(s.cfg, s.cache, s.chunks(max_chunk=hint), s.k, s.v, s.pos)
+        after.append(s.copies())
+    torch.cuda.synchronize()
+    assert not torch.equal(before[0], after[0][0])
+    for other in after[1:]:
+        assert all(a is None or torch.equal(a, b) for a, b in zip(after[0], other))
+
+
 @pytest.mark.parametrize("turn", [False, True])
 @pytest.mark.parametrize("store", STORES)
 @pytest.mark.parametrize("i", range(len(SHAPES)))

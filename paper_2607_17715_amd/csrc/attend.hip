@@ -222,18 +222,19 @@ __device__ inline bf16x8 bf16_of(const float (&x)[8]) {
                              pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
   return __builtin_bit_cast(bf16x8, u);
 }
-// x as two bf16 numbers, within 2^-16 of itself.  The first is cut short, so that the second has
-// its sign, and is never zero beside it (of 2^-94 and more; where the first says all, 2^-32 of it
-// stands in): an infinite key element then gives the one infinity that a single number gives, not
-// the NaN of infinity times zero or of two infinities of opposite sign.  An infinity stands in
-// both.
+// x as two bf16 numbers, within 2^-16 of itself.  The first is cut short and the second is what
+// that leaves and 2^-24 of the first, so that it has the first's sign and is never zero beside it
+// (of 2^-100 and more): an infinite key element then gives the one infinity that a single number
+// gives, not the NaN of infinity times zero or of two infinities of opposite sign.  An infinity
+// stands in both.
 __device__ inline void split_bf16(const float (&x)[8], bf16x8& hi, bf16x8& rest) {
+  constexpr float most = 0x1.fffffep127f;
   uint32_t w[4];
   float r[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const float h = __uint_as_float(__float_as_uint(x[e]) & 0xffff0000u);
-    r[e] = x[e] == h ? h * 0x1p-32f : x[e] - h;
+    r[e] = __builtin_fmaf(-__builtin_amdgcn_fmed3f(h, -most, most), 1.f - 0x1p-24f, x[e]);
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i)

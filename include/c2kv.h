@@ -376,11 +376,12 @@ c2kv_status c2kv_cache_read(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,
  * natural-log (NULL to skip).  A token that sees no key gets zeros and an lse of -inf; a
  * key whose score is -inf has no weight, and one of +inf or NaN makes its row NaN;
  * what lies in pages behind the last cached token has no effect, whatever it is.
- * Rounding, bf16 activations: probabilities to bf16 for their product with the values; the
- * turned and scaled query, where max_chunk * H_q / H_kv <= 128, to a sum of two bf16 numbers
- * (a score within 2^-16 of sum |q_i k_i|), and where it is more to one, as c2kv_attend does
- * (2^-8).  The same token may so come out differently beside a longer chunk or under another
- * bound, within these; equal calls give equal bits.
+ * Rounding, bf16 activations: the turned and scaled query, where max_chunk * H_q / H_kv <=
+ * 128, to a sum of two bf16 numbers (a score within 2^-16 of sum |q_i k_i|), and where it is
+ * more to one, as c2kv_attend does (2^-8); probabilities, for their product with the values,
+ * to two (within 2^-16) where max_chunk is 1 and H_q / H_kv at most 32, else to one (2^-8).
+ * The same token may so come out differently beside a longer chunk or under another bound,
+ * within these; equal calls give equal bits.
  * workspace: device memory on 256 bytes, of c2kv_cache_attend_workspace's size; calls
  * that share one must be ordered.  It need not be cleared.  out must not overlap q, nor
  * in any of these calls what is written what is read. */

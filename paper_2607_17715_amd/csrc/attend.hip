@@ -336,12 +336,12 @@ __device__ inline float infinity_of(float share, int sign) {
 // in flight (one where 32 rows leave no registers for the second).
 //
 // int8 codes become bf16 exactly; key scales multiply the scores, value scales the
-// probabilities, in fp32.  A turned query is held as two bf16 numbers, the second what the
-// first leaves: rounded to one, it would be the largest error of the output (queries of
-// standard deviation 2: 2-norm 0.0041 of the output's, 0.0024 with both, of which 0.0017 are
-// the output's own rounding).  Both come from LDS every step, and the MFMAs that the second
-// adds are idle time here.  Probabilities are rounded to bf16 for their product, as everywhere
-// in this library; their sum and the output stay in fp32.
+// probabilities, in fp32.  Turned queries and probabilities are held as two bf16 numbers each, the
+// second what the first leaves: the output is then off by its own rounding (2-norm of a batch's
+// error 0.0017 of the output's; with queries rounded to one 0.0041, with probabilities 0.0023, in
+// int8 0.0025).  Queries come from LDS every step, and the MFMAs that the second numbers add are
+// idle time here (24 requests of 1200 to 6200 tokens: 79.1 us with probabilities in one, 79.4 in
+// two; 512 of 200 to 900 in int8 181 and 184).  Sums and outputs stay in fp32.
 //
 // Bound by memory: with up to 16 rows 256 KB are in flight a CU (D = 128), and the rest hides under
 // them.  24 requests of 1200 to 6200 tokens (bf16, 373 MB) in pages of 128: 71 to 77 us, 5.2 to
@@ -520,7 +520,7 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
     auto compute = [&](int step, Set& x) __attribute__((always_inline)) {
       const int key0 = step * KS;
       const bool partial = key0 + KS > keys || x.page < 0;
-      bf16x8 pb[NB][U];
+      bf16x8 pb[NB][U], pr_rest[NB][U];
       f32x4 s[NB][2 * U];
 #pragma unroll
       for (int m = 0; m < 2 * U; ++m)
@@ -621,7 +621,7 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           const float (&x8)[8] = reinterpret_cast<const float (&)[8]>(pr[8 * u]);
-          pb[nb][u] = bf16_of(x8);
+          split_bf16(x8, pb[nb][u], pr_rest[nb][u]);
         }
       }
 #pragma unroll
@@ -632,8 +632,11 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttendParams a) {
           if constexpr (I8) vf = bf16_of_i8(x.v[db][2 * u], x.v[db][2 * u + 1]);
           else vf = __builtin_bit_cast(bf16x8, x.v[db]);
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
+          for (int nb = 0; nb < NB; ++nb) {
             o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pb[nb][u], o[nb][db], 0, 0, 0);
+            o[nb][db] =
+                __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pr_rest[nb][u], o[nb][db], 0, 0, 0);
+          }
         }
     };
     for (int step = s0 / SETS * SETS; step < s1; step += SETS) {

@@ -411,6 +411,38 @@ def test_bounds_choose_how_far_queries_are_rounded(hint, half, blocks, store):
     assert (err <= bound).all()
 
 
+@pytest.mark.parametrize("store", ["bf16", "i8"])
+@pytest.mark.parametrize("hq,d", [(8, 128), (8, 64), (48, 128)])
+def test_single_tokens_are_rounded_once(hq, d, store):
+    """A single token's output is its own rounding, 2^-8, away from fp32's: queries and
+    probabilities are within 2^-16.  A score is so off by at most 2^-16 of its products' magnitudes
+    (and 2^-20 for fp32), a weight by twice the largest such error and 2^-16, and so the output by
+    that of its weights' sum of magnitudes of values."""
+    s = Scene(store, [1, 1, 1], [2, 20, 90], hq=hq, hkv=2, d=d, seed=37)
+    out = s.out()
+    c2kv.c2kv_cache_attend(s.cfg, s.cache, s.chunks(), s.q, out)
+    torch.cuda.synchronize()
+    kp, vp = s.pages64()
+    q, G, got = f64(s.q), s.hq // s.hkv, f64(out)
+    most = 0.0
+    for b in range(s.B):
+        n = int(s.kv_len[b])
+        ids = s.table[b][:-(-n // s.page)]
+        k = np.concatenate([kp[i] for i in ids], 1)[:, :n]
+        v = np.concatenate([vp[i] for i in ids], 2)[:, :, :n]
+        for h in range(s.hq):
+            x = k[h // G] @ q[b, h] / s.d ** 0.5
+            off = (np.abs(k[h // G]) @ np.abs(q[b, h])).max() / s.d ** 0.5 * (2.0 ** -16 + 2.0 ** -20)
+            p = np.exp(x - x.max())
+            p /= p.sum()
+            ref, mag = v[h // G] @ p, np.abs(v[h // G]) @ p
+            bound = 2.0 ** -8 * np.abs(ref) + (2 * off + 2.0 ** -16 + 2.0 ** -20) * mag
+            err = np.abs(got[b, h] - ref)
+            most = max(most, float((err / bound).max()))
+            assert (err <= bound).all(), (b, h, most)
+    say(f"single tokens {store}: at most {most:.2f} of the bound")
+
+
 @pytest.mark.parametrize("store", STORES)
 def test_prime_groups_and_many_requests(store):
     """37 query heads a kv-head (no divisor up to 32), and 300 requests, some of them empty."""

@@ -379,7 +379,7 @@ c2kv_status c2kv_cache_read(const c2kv_attn_cfg* cfg, const c2kv_cache* cache,
  * Rounding, bf16 activations: the turned and scaled query, where max_chunk * H_q / H_kv <=
  * 128, to a sum of two bf16 numbers (a score within 2^-16 of sum |q_i k_i|), and where it is
  * more to one, as c2kv_attend does (2^-8); probabilities, for their product with the values,
- * to two (within 2^-16) where max_chunk is 1 and H_q / H_kv at most 32, else to one (2^-8).
+ * to two (within 2^-16) where max_chunk is 1 and H_q / H_kv at most 32, else to one at least.
  * The same token may so come out differently beside a longer chunk or under another bound,
  * within these; equal calls give equal bits.
  * workspace: device memory on 256 bytes, of c2kv_cache_attend_workspace's size; calls

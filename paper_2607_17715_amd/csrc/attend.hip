@@ -753,17 +753,24 @@ __device__ inline void wait_loads_barrier() {
 //
 // int8 codes go through registers.  Keys become bf16 exactly and their scales multiply the
 // scores in fp32; values are decoded there (code * scale in fp32) and rounded once, as
-// c2kv_compose rounds them.  (2048 tokens over 32k, 32 query heads: 1.30 ms.  Keys decoded and
-// rounded too: 1.14, but the 2-norm of the error is then 0.0052 of the output's, not 0.0045;
-// value scales applied to the probabilities instead: 1.35, and 0.0042.)
+// c2kv_compose rounds them.  (2048 tokens over 32k, 32 query heads: 1.20 to 1.30 ms, 0.95 to 0.87
+// PFLOP/s, and 26 us of joining: after a tile's barrier all wavefronts decode the next one while the
+// MFMAs, busy 41 % of the time, wait.  Keys decoded and rounded too: 12 % faster, but the 2-norm of
+// the error is then 0.0052 of the output's, not 0.0045; value scales applied to the probabilities
+// instead: 4 % slower, and 0.0042.)
 //
 // Bound by the MFMAs' share of a wavefront pair's time: 2048 tokens over 32k (64 query heads,
-// 2.27 TFLOP) in 2.03 ms, 1.12 PFLOP/s, where a library product of 8192 cubed reaches 1.21;
-// the MFMAs are busy 57 % of the time, the softmax and the operands' LDS reads the rest.  A
-// wavefront that runs the scores of one tile beside the softmax of the tile before spills;
+// 2.27 TFLOP) in 1.97 to 2.03 ms, 1.15 to 1.12 PFLOP/s, where a library product of 8192 cubed
+// reaches 1.21; the MFMAs are busy 57 % of the time, the softmax and the operands' LDS reads the
+// rest.  A wavefront that runs the scores of one tile beside the softmax of the tile before spills;
 // values' rows exchanged so that no LDS read meets a conflict (a third do) change nothing.
-// fp32: 1024 tokens over 1024, 32 heads, 259 us, 100 TFLOP/s of the 147 that a library product
-// of 4096 cubed reaches.
+// fp32: 1024 tokens over 1024, 32 heads, 239 to 268 us, 108 to 96 TFLOP/s of the 147 that a library
+// product of 4096 cubed reaches, the MFMAs busy 76 % of the time.
+//
+// Few rows over a long cache leave most wavefronts and the MFMAs idle (busy 16 %), and one workgroup
+// a CU nothing to hide a tile's chain under, about 2 us of barrier, LDS reads, products and softmax:
+// 81 drafts of 16 requests over 329 MB of bf16 take 87 us, over 171 MB of int8 95 to 100, single
+// fp32 tokens of 16 requests over 593 MB 317.
 template <typename T, typename S, int D, int RG>
 __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
   using M = Mma<T>;
@@ -776,7 +783,9 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
   // Queries held as two bf16 numbers, as for single tokens, where 128 rows a workgroup leave
   // the MFMAs idle (16 requests of 3 to 7 drafts: 81 -> 84 us).  256 rows would pay half as
   // many products again for the scores (2048 tokens over 32k: 1.06 -> 1.43 ms): there a turned
-  // and scaled query is rounded once, as c2kv_attend's are.
+  // and scaled query is rounded once, as c2kv_attend's are.  Probabilities are rounded once in
+  // both (two numbers in 128 rows: drafts' error 0.0022 -> 0.0017 of the output's 2-norm, 88 -> 91
+  // us with 32 query heads and 87 -> 95 with 64; int8 0.0027 -> 0.0023, 90 -> 102).
   constexpr bool TWO = !F32 && RG == 4;
   constexpr int NST = F32 || I8 ? 2 : TWO ? 3 : 4;   // tiles in LDS
   constexpr int LK = ST * W::CK / NTH, LV = D * W::CV / NTH, LPT = LK + LV;
@@ -1369,9 +1378,10 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendParams a) {
 // tokens: 5.5 us; an empty launch takes 4).  Blocks have many rows, and how many of them are
 // cut depends on the lengths: PW = 1, and all their rows, in one line, are shared evenly (512
 // rows of a kv-head over 4128 tokens, 16 pieces each: 30.0 us with workgroups for every share's
-// unit, cut or not, 10.1 so; 128 tokens over 100: 7.8 and 4.4; drafts 4.7 and 4.6; where most
-// shares are cut, finding the rows costs: 2048 tokens of 64 heads 20.6 and 25.4, of 150 us
-// before them.  1024 workgroups; 512: 36.5, 2048: the same, but drafts 6.3; 8192: 32.3).
+// unit, cut or not, 10.1 so; 128 tokens over 100: 7.8 and 4.4; drafts with 32 query heads 4.7 and
+// 4.6.  Where most shares are cut, finding the rows costs: drafts with 64 heads 6.4 and 6.0, 2048
+// tokens of 64 heads 20.6 and 25.4 of 150 us before them, over 32k 26.5 and 30.6 of 2.0 ms.  1024
+// workgroups; 512: 36.5, 2048: the same, but drafts 6.3; 8192: 32.3).
 template <typename T, int D, int RB, int PW>
 __global__ __launch_bounds__(256) void join_kernel(AttendParams a) {
   constexpr int CPL = D / 64, NW = 4, N = PW > 1 ? 16 : 8;   // columns of a lane; pieces in flight

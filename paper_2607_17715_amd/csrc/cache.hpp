@@ -1,5 +1,5 @@
 // The growing paged cache: parameters of its kernels and their launchers (defined in
-// cache.hip), called by the C ABI in api.cpp.  Non-null events are stamped at the
+// cache.hip, those of attention in attend.hip), called by the C ABI in api.cpp.  Non-null events are stamped at the
 // kernel's start and end.
 #pragma once
 

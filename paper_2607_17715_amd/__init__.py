@@ -299,6 +299,16 @@ class Plan:
         return self
 
 
+def _check_scales(code: int, shape, float32, *scales):
+    """Scales of a pool of rows `shape`, tensors or arrays.  (Of other than int8 pools the library
+    reads none.)"""
+    for s in scales:
+        if code == C2KV_I8 and s is not None and (s.dtype != float32 or
+                                                  tuple(s.shape) != tuple(shape[:2])):
+            raise ValueError(f"pool scales must be float32 {list(shape[:2])}, got {s.dtype} "
+                             f"{list(s.shape)}")
+
+
 def pool_desc(k, v, k_scale=None, v_scale=None) -> PoolDesc:
     """A pool of rows k and v [n_rows][H_kv][D], for int8 with float32 scales [n_rows][H_kv],
     all on one device.  The descriptor keeps the tensors that it points to."""
@@ -307,11 +317,7 @@ def pool_desc(k, v, k_scale=None, v_scale=None) -> PoolDesc:
     if v.dtype != k.dtype or v.shape != k.shape:
         raise ValueError("pool K and V must have the same dtype and shape")
     tensors = (k, v, k_scale, v_scale)
-    if code == C2KV_I8:                        # (of other pools the library reads no scales)
-        for s in tensors[2:]:
-            if s is not None and (s.dtype != torch.float32 or s.shape != k.shape[:2]):
-                raise ValueError(f"pool scales must be float32 {list(k.shape[:2])}, got {s.dtype} "
-                                 f"{list(s.shape)}")
+    _check_scales(code, k.shape, torch.float32, k_scale, v_scale)
     _one_device(*tensors)
     desc = PoolDesc(code, *(_dev_ptr(t) for t in tensors), int(k.shape[0]))
     desc.tensors, desc.row_shape, desc.dev = tensors, tuple(k.shape[1:]), k.get_device()
@@ -578,9 +584,14 @@ class HostPool:
         code = {"f32": C2KV_F32, "bf16": C2KV_BF16, "i8": C2KV_I8}[dtype]
         if pool_k.shape != pool_v.shape:
             raise ValueError("pool K and V must have the same shape")
+        size = {"f32": 4, "bf16": 2, "i8": 1}[dtype]
+        if pool_k.itemsize != size or pool_v.itemsize != size:
+            raise ValueError(f"{dtype} storage has {size} bytes an element")
+        _check_scales(code, pool_k.shape, np.float32, k_scale, v_scale)
         self.nbytes = 0
         ptrs = [self._put(a) for a in (pool_k, pool_v, k_scale, v_scale)]
         self.desc = PoolDesc(code, ptrs[0], ptrs[1], ptrs[2], ptrs[3], int(pool_k.shape[0]))
+        self.desc.row_shape = tuple(pool_k.shape[1:])
 
     def _put(self, a: Optional[np.ndarray]):
         if a is None:

@@ -272,6 +272,19 @@ def test_binding_refuses_pools_over_two_devices(monkeypatch, i):
         c2kv.pool_desc(*t)
 
 
+def test_host_pool_knows_its_rows(monkeypatch):
+    """c2kv_pool_write writes into a host pool as into one on the device."""
+    monkeypatch.setattr(c2kv.HostPool, "_put", lambda self, a: P)
+    k, sc = np.zeros((7, 2, 64), np.int8), np.ones((7, 2), np.float32)
+    assert c2kv.HostPool(k, k, "i8", sc, sc).desc.row_shape == (2, 64)
+    for bad in (sc.astype(np.float16), sc[:6], sc[:, 0]):
+        with pytest.raises(ValueError, match="scales"):
+            c2kv.HostPool(k, k, "i8", sc, bad)
+    for dtype in ("f32", "bf16"):
+        with pytest.raises(ValueError, match="bytes an element"):
+            c2kv.HostPool(k, k, dtype)
+
+
 def test_pool_descriptor_keeps_its_tensors(monkeypatch):
     """Its pointers must not outlive what they point to."""
     monkeypatch.setattr(c2kv, "_dev_ptr", lambda t: t.data_ptr())

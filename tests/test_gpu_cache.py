@@ -699,6 +699,50 @@ def test_attend_keys_that_are_not_finite(n, hq, hint, store):
     assert torch.equal(out[:n[0], G:], was[:n[0], G:])
 
 
+@pytest.mark.parametrize("n,hq,hint", [([1, 1], 8, 1), ([1, 1], 80, 1), ([5, 3], 8, 5),
+                                       ([90, 40], 8, 90)])
+def test_attend_int8_key_scales_that_are_nan(n, hq, hint):
+    """The scale of a cached key that held an infinity or a NaN: rows that see it are NaN, and
+    no others."""
+    s = Scene("i8", n, [70, 130], hq=hq, hkv=2, seed=24)
+    say(f"key scales not finite {n} {hq}")
+    G, t = hq // 2, n[0] // 2
+    ch = s.chunks(max_chunk=hint)
+    out, lse = s.out(), s.lse()
+    c2kv.c2kv_cache_attend(s.cfg, s.cache, ch, s.q, out, s.pos, lse)
+    where = cache_oracle.places(s.tok_off, s.kv_len, s.table, s.page, s.n_pages, s.n_tokens)
+    s.ks[where[t][2], 1, where[t][3]] = float("nan")
+    out2, lse2 = s.out(), s.lse()
+    c2kv.c2kv_cache_attend(s.cfg, s.cache, ch, s.q, out2, s.pos, lse2)
+    torch.cuda.synchronize()
+    assert torch.isnan(out2[t:n[0], G:]).all() and torch.isnan(lse2[t:n[0], G:]).all()
+    out2[t:n[0], G:], lse2[t:n[0], G:] = out[t:n[0], G:], lse[t:n[0], G:]
+    assert torch.equal(out, out2) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("hq", [8, 48])
+def test_single_tokens_see_values_that_are_not_finite(hq, store):
+    """An infinite value makes its column infinite, whatever the weights, a NaN makes it NaN."""
+    s = Scene(store, [1, 1], [70, 130], hq=hq, hkv=2, seed=25)
+    ch, G, inf = s.chunks(), hq // 2, float("inf")
+    out = s.out()
+    c2kv.c2kv_cache_attend(s.cfg, s.cache, ch, s.q, out, s.pos)
+    want = out.clone()
+    page = s.table[0, 0]
+    if store == "i8":
+        s.vs[page, 1, 9] = float("nan")
+        want[0, G:] = float("nan")
+    else:
+        s.vp[page, 0, 3, 5], s.vp[page, 0, 4, 6], s.vp[page, 1, 7, 9] = inf, -inf, float("nan")
+        want[0, :G, 3], want[0, :G, 4], want[0, G:, 7] = inf, -inf, float("nan")
+    out2 = s.out()
+    c2kv.c2kv_cache_attend(s.cfg, s.cache, ch, s.q, out2, s.pos)
+    torch.cuda.synchronize()
+    assert torch.equal(torch.isnan(out2), torch.isnan(want))
+    assert torch.equal(out2.nan_to_num(0, inf, -inf), want.nan_to_num(0, inf, -inf))
+
+
 @pytest.mark.parametrize("store", STORES)
 @pytest.mark.parametrize("n,hint", [([1, 1], 1), ([5, 3], 5), ([100, 40], 100)])
 def test_attend_infinite_queries(n, hint, store):

@@ -52,8 +52,8 @@ __device__ inline int page_of(const ChunkView& c, const PageView& p, int b, int 
 // cos and sin of pos positions' turn of a pair: the angle in whole turns is formed and
 // reduced in 64 bits (a far position times a frequency loses its fraction in 32), and the
 // instructions take it in turns (within 2^-22.9 over [-1/2, 1/2], measured at 2^20 angles, and
-// within 2^-22 with the rounding of the reduced angle; a plan's tables are within 2^-25, but a
-// polynomial of that precision would cost a long fp32 write some 5 of its 59 us).
+// within 2^-22 with the rounding of the reduced angle; a plan's tables are within 2^-25, but that
+// takes polynomials in 64 bits, about 25 operations an angle, which have not been tried here).
 __device__ inline void turn_cs(int pos, double turns, float& c, float& s) {
   double x = pos * turns;
   x -= __builtin_rint(x);
